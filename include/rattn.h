@@ -418,6 +418,151 @@ int rattn_qk_prologue_backward(const rattn_qk_params* p, const void* dq_out, con
 size_t rattn_qk_prologue_workspace_bytes(int B, int H_q, int H_kv, int T, int d);
 int rattn_qk_prologue_status(void* stream);
 
+/*
+ * Speculative decoding on the ring and the state.  The paper decodes token by token; a server that lets a
+ * small model draft several tokens ahead needs the same layer for a tree of drafted tokens at once, without
+ * touching the cache (a running sum cannot be taken back), the decision which of them stand, and the entry of
+ * those into the cache:
+ *
+ *     rattn_draft_attention   every layer: all nodes of the tree, each as if its path had been decoded
+ *     rattn_draft_verify      once: the accepted path and the token drawn behind it
+ *     rattn_draft_commit      every layer: the accepted path's keys and values enter ring and state
+ *
+ * The tree.  `parents` (device int32 [B,N]) gives every node its parent: -1 for a node that follows the cached
+ * tokens directly, else the index of an earlier node (parents[b][i] < i).  A node whose parent is neither, or is
+ * itself no node, is no part of the tree (-2 marks what a batch entry does not use).  A node at depth e (depth 0:
+ * parent -1) sits at sequence position pos + e.  At most RATTN_DRAFT_MAX_NODES nodes.
+ */
+#define RATTN_DRAFT_MAX_NODES 128
+
+/*
+ * Parameter block of rattn_draft_attention and rattn_draft_commit.  Zero-initialise it, then fill in.
+ *   q, out       [B,H_q,N,d]     k, v  [B,H_kv,N,d]     (with RATTN_LAYOUT_BTHD: [B,N,H,d])
+ *   k_ring, v_ring [B,H_kv,w,d], state [B,H_kv,d,d] fp32, pos: as for rattn_decode_step: the ring holds the tokens
+ *                pos-w .. pos-1 (those >= 0) at slot j % w, the state those before.
+ *   pos_dev      optional device int32 [B], a position per batch entry (overrides pos).  Positions are at least 0 and,
+ *                with the deepest node's depth, at most 2^31 - 1 - w.
+ *   path, n_accepted   rattn_draft_commit only, as rattn_draft_verify writes them.
+ * dtype, scale, eps, gains, feature_map, layout and flags (RATTN_FLAG_FORCE_GENERIC) as in rattn_params.  Every
+ * combination of dtype, d, w and group is supported; accumulation, softmax, feature map and norms are fp32, and the bf16
+ * kernels put no restriction on the range of v.
+ */
+typedef struct rattn_draft_params {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  const int32_t* parents;
+  void* k_ring;                  /* read by rattn_draft_attention, updated by rattn_draft_commit */
+  void* v_ring;
+  float* state;
+  int32_t B, H_q, H_kv, N, d, w;
+  int32_t dtype;                 /* rattn_dtype */
+  int32_t feature_map;           /* rattn_feature_map */
+  int32_t layout;                /* rattn_layout of q, k, v, out */
+  uint32_t flags;
+  float scale;
+  float eps;
+  const float* gamma_swa;
+  const float* gamma_rla;
+  const int32_t* pos_dev;
+  const int32_t* path;
+  const int32_t* n_accepted;
+  int32_t pos;
+} rattn_draft_params;
+
+/*
+ * For every node of the tree: softmax attention over the last w + 1 tokens up to and including the node -- of the ring,
+ * then of the node's path -- plus the linear branch over all earlier ones (state, ring tokens and path nodes that have
+ * left the node's window), combined as in rattn_forward: what rattn_decode_step would give at the end of the node's
+ * path.  Nodes off a node's path have no influence on it, whatever their keys and values hold.  Rows of out that belong to no
+ * node are left as they were.  Cache and state are only read.
+ */
+int rattn_draft_attention(const rattn_draft_params* p, void* stream);
+
+/*
+ * Enters the accepted tokens into the cache, as n_accepted[b] steps of rattn_decode_step would: token a of the path
+ * (node path[b][a] of k, v) takes position pos + a, ring slot (pos + a) % w, and the token that leaves the window,
+ * pos + a - w if that is >= 0, is folded into the state.  n_accepted[b] = 0 leaves entry b as it is; a path entry outside
+ * 0 .. N-1 ends the path.  Uses k, v, path, n_accepted, rings, state, pos, sizes, dtype, feature_map, layout;
+ * H_q, scale, eps and the rest are not looked at.  Ring and state are updated in place; positions are the caller's to advance.
+ */
+int rattn_draft_commit(const rattn_draft_params* p, void* stream);
+
+/* RATTN_ERR_TIMEOUT if a bounded device-side wait has expired in any of the draft calls on the current device since it
+ * was last asked (synchronises the stream), else RATTN_OK. */
+int rattn_draft_status(void* stream);
+
+/*
+ * Verification of the tree against the target's probabilities, from given random numbers: the accepted tokens and the one
+ * drawn behind them are distributed as if the target had been sampled token by token.
+ *
+ * Node 0 is the token sampled last (parent -1; any other parent: the entry is idle and gets n_accepted 0, token -1).  Nodes
+ * are looked at in index order; node i is tested when its parent is the node accepted last, c.  With p the row of c in
+ * target_probs, q its row in draft_probs (the distribution from which c's children were drawn, independently of each
+ * other) and x = tokens[i], the test is
+ *
+ *     u[i] q(x) Z < r(x)      where r = p, Z = 1 at the first test under c;
+ *
+ * if it holds, i is accepted (c = i).  If not, r becomes max(r - Z q, 0) and Z the sum of that, unless less than 2^-40 of Z
+ * would be left (then r and Z stay).  draft_probs = NULL: children were not drawn but chosen; q(x) counts as 1 in the test, and
+ * a rejection sets r(x) to 0 and takes it off Z.  Behind the last test the token is the lowest x whose sum r(0) + .. + r(x)
+ * exceeds u[0] times the sum of r (of p, if r sums to 0; -1 if p does too).
+ *
+ *   tokens, parents   device int32 [B,N]; a token outside 0 .. V-1 is rejected and takes nothing off r
+ *   target_probs      [B,N,V] in dtype (rattn_dtype): row i is the target's distribution behind node i.  Rows that no test and
+ *                     no draw asks for are not read.  Probabilities that are negative or NaN count as 0.
+ *   draft_probs       [B,N,V] in dtype, or NULL
+ *   u                 fp32 [B,N] uniform in [0, 1)
+ *   path              int32 [B,N] out: the accepted nodes from node 0 on, then -1
+ *   n_accepted        int32 [B] out: how many
+ *   token             int32 [B] out: the token drawn behind them
+ * Sums and comparisons are fp64.  Tokens are not sorted, probabilities not renormalised.
+ */
+typedef struct rattn_verify_params {
+  const int32_t* tokens;
+  const int32_t* parents;
+  const void* target_probs;
+  const void* draft_probs;
+  const float* u;
+  int32_t* path;
+  int32_t* n_accepted;
+  int32_t* token;
+  int32_t B, N, V;
+  int32_t dtype;                 /* rattn_dtype */
+} rattn_verify_params;
+
+int rattn_draft_verify(const rattn_verify_params* p, void* stream);
+
+/*
+ * rattn_qk_prologue for tokens whose place is given by several numbers, or whose positions are not consecutive: a video's
+ * tokens (time, height, width), an image's, the nodes of a tree of drafts (one axis: the node's position).
+ *   at         device int32 [n_axes,B,T]: coordinate of every token on every axis
+ *   n_axes     1 .. 4
+ *   sections   rotated pairs of each axis, at least 1 each; their sum is at most d/2, and pairs beyond it are not rotated
+ *   order      which pairs those are, and with which frequencies:
+ *                RATTN_AXES_RUNS   the first sections[0] pairs belong to axis 0, the next to axis 1, ...; pair i turns by
+ *                                  at * theta^(-2i/d), as in rattn_qk_prologue
+ *                RATTN_AXES_OWN    the same runs; pair j of an axis' own s turns by at * theta^(-j/s)
+ *                RATTN_AXES_DEALT  pairs go to the axes in turn (0, 1, .., 0, 1, ..), an axis that has its number is
+ *                                  passed over; pair i turns by at * theta^(-2i/d)
+ * The block's pos0 must be 0 and its pos NULL, theta > 0.  Everything else, the backward and its workspace
+ * included, as for rattn_qk_prologue and rattn_qk_prologue_backward; rattn_qk_prologue_status covers both.
+ */
+typedef enum rattn_axes_order { RATTN_AXES_RUNS = 0, RATTN_AXES_OWN = 1, RATTN_AXES_DEALT = 2 } rattn_axes_order;
+
+typedef struct rattn_qk_axes {
+  const int32_t* at;
+  int32_t n_axes;
+  int32_t sections[4];
+  int32_t order;                 /* rattn_axes_order */
+} rattn_qk_axes;
+
+int rattn_qk_prologue_axes(const rattn_qk_params* p, const rattn_qk_axes* axes, void* stream);
+int rattn_qk_prologue_axes_backward(const rattn_qk_params* p, const rattn_qk_axes* axes, const void* dq_out,
+                                    const void* dk_out, void* dq, void* dk, float* dq_gain, float* dk_gain,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

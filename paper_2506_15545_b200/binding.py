@@ -24,6 +24,8 @@ MODE_RATTN, MODE_SWA_ONLY, MODE_FULL_CAUSAL = 0, 1, 2
 FLAG_FORCE_GENERIC, FLAG_SAVE_RESIDUALS = 1, 2
 PHI_SOFTMAX, PHI_RELU, PHI_IDENTITY = 0, 1, 2
 LAYOUT_BHTD, LAYOUT_BTHD = 0, 1
+AXES_RUNS, AXES_OWN, AXES_DEALT = 0, 1, 2
+DRAFT_MAX_NODES = 128
 
 EXPORTS = (
     "rattn_forward", "rattn_forward_ex", "rattn_backward", "rattn_backward_ex",
@@ -33,6 +35,8 @@ EXPORTS = (
     "rattn_uses_tensor_path", "rattn_timing_enable", "rattn_timing_read",
     "rattn_forward_static", "rattn_static_status", "rattn_tune",
     "rattn_qk_prologue", "rattn_qk_prologue_backward", "rattn_qk_prologue_workspace_bytes", "rattn_qk_prologue_status", "rattn_decode_status", "rattn_forward_status",
+    "rattn_qk_prologue_axes", "rattn_qk_prologue_axes_backward", "rattn_draft_attention", "rattn_draft_commit",
+    "rattn_draft_verify", "rattn_draft_status",
 )
 TUNE_STATE_STRIDE, TUNE_OVERLAP, TUNE_UNIT_ORDER, TUNE_GRID, TUNE_DECODE_STAGES, TUNE_STATE_PROGRESS = 0, 1, 2, 3, 4, 5
 
@@ -67,6 +71,34 @@ class RattnQkParams(ctypes.Structure):
         ("T", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("eps", ctypes.c_float), ("theta", ctypes.c_float),
         ("pos0", ctypes.c_int32), ("layout", ctypes.c_int32), ("pos", ctypes.c_void_p),
+    ]
+
+
+class RattnQkAxes(ctypes.Structure):
+    _fields_ = [
+        ("at", ctypes.c_void_p), ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4), ("order", ctypes.c_int32),
+    ]
+
+
+class RattnDraftParams(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p),
+        ("parents", ctypes.c_void_p), ("k_ring", ctypes.c_void_p), ("v_ring", ctypes.c_void_p),
+        ("state", ctypes.c_void_p),
+        ("B", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("N", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("w", ctypes.c_int32), ("dtype", ctypes.c_int32), ("feature_map", ctypes.c_int32),
+        ("layout", ctypes.c_int32), ("flags", ctypes.c_uint32), ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+        ("gamma_swa", ctypes.c_void_p), ("gamma_rla", ctypes.c_void_p), ("pos_dev", ctypes.c_void_p),
+        ("path", ctypes.c_void_p), ("n_accepted", ctypes.c_void_p), ("pos", ctypes.c_int32),
+    ]
+
+
+class RattnVerifyParams(ctypes.Structure):
+    _fields_ = [
+        ("tokens", ctypes.c_void_p), ("parents", ctypes.c_void_p), ("target_probs", ctypes.c_void_p),
+        ("draft_probs", ctypes.c_void_p), ("u", ctypes.c_void_p), ("path", ctypes.c_void_p),
+        ("n_accepted", ctypes.c_void_p), ("token", ctypes.c_void_p),
+        ("B", ctypes.c_int32), ("N", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
     ]
 
 
@@ -140,6 +172,19 @@ def lib() -> ctypes.CDLL:
     L.rattn_decode_status.restype = ci
     L.rattn_qk_prologue_status.argtypes = [vp]
     L.rattn_qk_prologue_status.restype = ci
+    L.rattn_qk_prologue_axes.argtypes = [ctypes.POINTER(RattnQkParams), ctypes.POINTER(RattnQkAxes), vp]
+    L.rattn_qk_prologue_axes.restype = ci
+    L.rattn_qk_prologue_axes_backward.argtypes = [ctypes.POINTER(RattnQkParams), ctypes.POINTER(RattnQkAxes), vp, vp, vp,
+                                                  vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.rattn_qk_prologue_axes_backward.restype = ci
+    L.rattn_draft_attention.argtypes = [ctypes.POINTER(RattnDraftParams), vp]
+    L.rattn_draft_attention.restype = ci
+    L.rattn_draft_commit.argtypes = [ctypes.POINTER(RattnDraftParams), vp]
+    L.rattn_draft_commit.restype = ci
+    L.rattn_draft_verify.argtypes = [ctypes.POINTER(RattnVerifyParams), vp]
+    L.rattn_draft_verify.restype = ci
+    L.rattn_draft_status.argtypes = [vp]
+    L.rattn_draft_status.restype = ci
     L.rattn_timing_enable.argtypes = [ci]
     L.rattn_timing_enable.restype = ci
     L.rattn_timing_read.argtypes = [ctypes.c_char_p, ctypes.c_size_t]
@@ -153,7 +198,8 @@ _native = None
 # in the order of native.cpp's table of entry points
 _ENTRIES = ("rattn_forward", "rattn_forward_static", "rattn_forward_ex", "rattn_backward", "rattn_backward_ex",
             "rattn_decode_step", "rattn_decode_step_ex", "rattn_qk_prologue", "rattn_qk_prologue_backward",
-            "rattn_qk_prologue_workspace_bytes")
+            "rattn_qk_prologue_workspace_bytes", "rattn_qk_prologue_axes", "rattn_qk_prologue_axes_backward",
+            "rattn_draft_attention", "rattn_draft_commit", "rattn_draft_verify")
 
 
 def native():
@@ -376,3 +422,47 @@ def rattn_qk_prologue_backward(q, k, dq_out, dk_out, *, q_gain=None, k_gain=None
     forward pass) and, with gain_grads, to the two gains.  Returns (dq, dk, dq_gain, dk_gain)."""
     return (_native or native()).qk_prologue_backward(
         q, k, dq_out, dk_out, q_gain, k_gain, theta, eps, pos0, pos, layout, gain_grads, workspace, stream)
+
+
+def rattn_qk_prologue_axes(q, k, at, sections, *, order=AXES_RUNS, q_gain=None, k_gain=None, theta=5.0e5, eps=1e-6,
+                           inplace=False, layout=LAYOUT_BHTD, stream=None):
+    """rattn_qk_prologue_axes: the prologue for tokens with a coordinate on each of 1 to 4 axes: at int32 [n_axes,B,T],
+    sections the rotated pairs of each axis, order one of AXES_RUNS, AXES_OWN, AXES_DEALT.  k may be None."""
+    return (_native or native()).qk_prologue_axes(q, k, at, sections, order, q_gain, k_gain, theta, eps, layout, inplace,
+                                                  stream)
+
+
+def rattn_qk_prologue_axes_backward(q, k, dq_out, dk_out, at, sections, *, order=AXES_RUNS, q_gain=None, k_gain=None,
+                                    theta=5.0e5, eps=1e-6, gain_grads=True, workspace=None, layout=LAYOUT_BHTD,
+                                    stream=None):
+    """rattn_qk_prologue_axes_backward: as rattn_qk_prologue_backward.  Returns (dq, dk, dq_gain, dk_gain)."""
+    return (_native or native()).qk_prologue_axes_backward(q, k, dq_out, dk_out, at, sections, order, q_gain, k_gain, theta,
+                                                           eps, layout, gain_grads, workspace, stream)
+
+
+def rattn_draft_attention(q, k, v, parents, k_ring, v_ring, state, pos=0, *, scale=1.0, eps=1e-6, gamma_swa=None,
+                          gamma_rla=None, out=None, phi=PHI_SOFTMAX, pos_dev=None, layout=LAYOUT_BHTD, flags=0,
+                          stream=None):
+    """rattn_draft_attention: the layer for a tree of N drafted tokens, q [B,H_q,N,d], k, v [B,H_kv,N,d] (or [B,N,H,d]),
+    parents int32 [B,N].  Ring and state are read only.  pos_dev: optional int32 [B] (then `pos` is ignored).  Rows of
+    `out` that belong to no node are left as they were (uninitialised where `out` is not given)."""
+    return (_native or native()).draft_attention(q, k, v, parents, k_ring, v_ring, state, pos, scale, eps, gamma_swa,
+                                                 gamma_rla, out, phi, pos_dev, layout, flags, stream)
+
+
+def rattn_draft_verify(tokens, parents, target_probs, draft_probs, u, stream=None):
+    """rattn_draft_verify: tokens, parents int32 [B,N], target_probs [B,N,V], draft_probs the same or None (drafts taken
+    greedily), u fp32 [B,N].  Returns (path int32 [B,N], n_accepted int32 [B], token int32 [B])."""
+    return (_native or native()).draft_verify(tokens, parents, target_probs, draft_probs, u, stream)
+
+
+def rattn_draft_commit(k, v, path, n_accepted, k_ring, v_ring, state, pos=0, *, phi=PHI_SOFTMAX, pos_dev=None,
+                       layout=LAYOUT_BHTD, flags=0, stream=None):
+    """rattn_draft_commit: the accepted path's keys and values enter ring and state, in place.  The caller then advances
+    its positions by n_accepted."""
+    (_native or native()).draft_commit(k, v, path, n_accepted, k_ring, v_ring, state, pos, phi, pos_dev, layout, flags, stream)
+
+
+def rattn_draft_status(stream=None) -> int:
+    """RATTN_ERR_TIMEOUT if a bounded wait expired in a draft call since the last query."""
+    return int(lib().rattn_draft_status(_stream(stream)))

@@ -1,0 +1,69 @@
+// Shared by the kernels of speculative decoding (draft*.cu): arguments, the tree of drafts, where a node's tensors lie.
+#pragma once
+
+#include "rattn_internal.h"
+
+namespace rattn {
+namespace draft {
+
+constexpr int kMaxNodes = RATTN_DRAFT_MAX_NODES;
+
+struct DraftArgs {
+  const void* q; const void* k; const void* v; void* out;
+  const int* parents;
+  void* k_ring; void* v_ring; float* state;
+  const float* gamma_swa; const float* gamma_rla;
+  const int* pos_dev; const int* path; const int* n_accepted;
+  int B, H_q, H_kv, N, d, w, group, dtype, phi, layout, pos;
+  unsigned flags;
+  float scale, eps;
+};
+
+// Element offset of node n of head h (of H) of batch entry b in a tensor of nodes.
+__device__ __forceinline__ size_t node_at(const DraftArgs& a, int b, int h, int H, int n) {
+  return (a.layout == RATTN_LAYOUT_BHTD ? ((size_t)b * H + h) * a.N + n : ((size_t)b * a.N + n) * H + h) * a.d;
+}
+__device__ __forceinline__ int entry_pos(const DraftArgs& a, int b) { return a.pos_dev ? max(a.pos_dev[b], 0) : a.pos; }
+
+// Ring slots by age.  The slot that position pos would take is pos % w; slot s holds token pos - w + rank(s), which exists
+// for rank >= w - min(pos, w).  A node at depth e sees the slots of rank >= e in its window and those below through the
+// linear branch.
+struct RingAge {
+  int w, head, first;            // head: pos % w; first: lowest rank that holds a token
+  __device__ __forceinline__ RingAge(int pos, int w_) : w(w_), head(pos % w_), first(pos < w_ ? w_ - pos : 0) {}
+  __device__ __forceinline__ int rank(int slot) const { return slot >= head ? slot - head : slot - head + w; }
+  __device__ __forceinline__ int slot(int rank) const { return rank + head >= w ? rank + head - w : rank + head; }
+};
+
+// Depth of node i, or -1 where it is no part of the tree.  par: the entry's parents in shared memory.  Chains of parents
+// fall strictly, so the walk ends.
+__device__ __forceinline__ int node_depth(const int* par, int i) {
+  int e = 0;
+  for (;;) {
+    const int p = par[i];
+    if (p == -1) return e;
+    if (p < 0 || p >= i) return -1;
+    i = p;
+    ++e;
+  }
+}
+
+// One bit per node: the node itself and its ancestors.
+struct NodeSet { uint32_t w[kMaxNodes / 32]; };
+__device__ __forceinline__ void node_path(const int* par, int i, NodeSet* s) {
+#pragma unroll
+  for (int j = 0; j < kMaxNodes / 32; ++j) s->w[j] = 0u;
+  for (;;) {
+#pragma unroll
+    for (int j = 0; j < kMaxNodes / 32; ++j) s->w[j] |= (i >> 5) == j ? 1u << (i & 31) : 0u;
+    const int p = par[i];
+    if (p < 0 || p >= i) return;
+    i = p;
+  }
+}
+
+cudaError_t launch_generic(const DraftArgs& a, cudaStream_t s);
+cudaError_t launch_commit(const DraftArgs& a, cudaStream_t s);
+
+}  // namespace draft
+}  // namespace rattn

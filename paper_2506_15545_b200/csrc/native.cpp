@@ -12,9 +12,12 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <climits>
 #include <cstring>
+#include <vector>
 
 #include "rattn.h"
 
@@ -31,6 +34,11 @@ struct Entry {
   decltype(&rattn_qk_prologue) qk_prologue;
   decltype(&rattn_qk_prologue_backward) qk_prologue_backward;
   decltype(&rattn_qk_prologue_workspace_bytes) qk_prologue_workspace_bytes;
+  decltype(&rattn_qk_prologue_axes) qk_prologue_axes;
+  decltype(&rattn_qk_prologue_axes_backward) qk_prologue_axes_backward;
+  decltype(&rattn_draft_attention) draft_attention;
+  decltype(&rattn_draft_commit) draft_commit;
+  decltype(&rattn_draft_verify) draft_verify;
 } E;
 PyObject* g_error = nullptr;                 // RattnError(code, where)
 
@@ -384,12 +392,233 @@ PyObject* qk_prologue_backward(Args a) {
   return Py_BuildValue("(NNNN)", wrap(dq), wrap(dk), wrap(dqg), wrap(dkg));
 }
 
+// ---- calls that check what they are given: type, shape and device of every tensor.  A call runs on the device of its tensors.
+void expect(const at::Tensor& t, at::ScalarType type, at::IntArrayRef sizes, const at::Tensor& first, const char* what) {
+  if (!t.defined()) return;
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s has the wrong dtype", what);
+    throw Raised{};
+  }
+  if (t.sizes() != sizes) {
+    PyErr_Format(PyExc_ValueError, "%s has the wrong shape", what);
+    throw Raised{};
+  }
+  if (t.device() != first.device()) {
+    PyErr_Format(PyExc_ValueError, "%s is on another device", what);
+    throw Raised{};
+  }
+}
+
+// Nodes [B, H, N, d] or [B, N, H, d] and what attention and commit share; read in the order of the binding.
+struct Draft {
+  rattn_draft_params p;
+  at::Tensor k, v, k_ring, v_ring, state, pos;
+  std::vector<int64_t> nodes(int64_t H) const {
+    if (p.layout == RATTN_LAYOUT_BTHD) return {p.B, p.N, H, p.d};
+    return {p.B, H, p.N, p.d};
+  }
+};
+void fill_draft(Draft* x) {
+  rattn_draft_params& p = x->p;
+  need_dim(x->k, 4);
+  need_dim(x->k_ring, 4);
+  const int hd = p.layout == RATTN_LAYOUT_BTHD ? 2 : 1;
+  p.B = (int32_t)x->k.size(0); p.H_kv = (int32_t)x->k.size(hd); p.N = (int32_t)x->k.size(3 - hd); p.d = (int32_t)x->k.size(3);
+  p.w = (int32_t)x->k_ring.size(2);
+  p.dtype = dtype_code(x->k);
+  const at::ScalarType type = x->k.scalar_type();
+  expect(x->v, type, x->k.sizes(), x->k, "v");
+  expect(x->k_ring, type, {p.B, p.H_kv, p.w, p.d}, x->k, "k_ring");
+  expect(x->v_ring, type, {p.B, p.H_kv, p.w, p.d}, x->k, "v_ring");
+  expect(x->state, at::kFloat, {p.B, p.H_kv, p.d, p.d}, x->k, "state");
+  expect(x->pos, at::kInt, {p.B}, x->k, "pos_dev");
+  p.k = ptr(x->k); p.v = ptr(x->v);
+  p.k_ring = ptr(x->k_ring); p.v_ring = ptr(x->v_ring); p.state = ptr<float>(x->state);
+  p.pos_dev = ptr<int32_t>(x->pos);
+}
+
+PyObject* draft_attention(Args a) {
+  Draft x;
+  std::memset(&x.p, 0, sizeof(x.p));
+  const at::Tensor q = a.tensor();
+  x.k = a.tensor(); x.v = a.tensor();
+  const at::Tensor parents = a.tensor();
+  x.k_ring = a.tensor(); x.v_ring = a.tensor(); x.state = a.tensor();
+  x.p.pos = a.i32();
+  x.p.scale = a.real();
+  x.p.eps = a.real();
+  const at::Tensor gs = a.maybe(), gr = a.maybe(), given = a.maybe();
+  x.p.feature_map = a.i32();
+  x.pos = a.maybe();
+  x.p.layout = a.i32();
+  x.p.flags = (uint32_t)a.i32();
+  const c10::DeviceGuard guard(q.device());
+  void* s = a.stream();
+  fill_draft(&x);
+  need_dim(q, 4);
+  x.p.H_q = (int32_t)q.size(x.p.layout == RATTN_LAYOUT_BTHD ? 2 : 1);
+  expect(q, x.k.scalar_type(), x.nodes(x.p.H_q), x.k, "q");
+  expect(parents, at::kInt, {x.p.B, x.p.N}, x.k, "parents");
+  expect(gs, at::kFloat, {x.p.H_q, x.p.d}, x.k, "gamma_swa");
+  expect(gr, at::kFloat, {x.p.H_q, x.p.d}, x.k, "gamma_rla");
+  expect(given, q.scalar_type(), q.sizes(), x.k, "out");
+  const at::Tensor out = or_like(given, q);
+  x.p.q = ptr(q); x.p.out = ptr(out); x.p.parents = ptr<int32_t>(parents);
+  x.p.gamma_swa = ptr<float>(gs); x.p.gamma_rla = ptr<float>(gr);
+  check(released([&] { return E.draft_attention(&x.p, s); }), "rattn_draft_attention");
+  return wrap(out);
+}
+
+PyObject* draft_commit(Args a) {
+  Draft x;
+  std::memset(&x.p, 0, sizeof(x.p));
+  x.k = a.tensor(); x.v = a.tensor();
+  const at::Tensor path = a.tensor(), n = a.tensor();
+  x.k_ring = a.tensor(); x.v_ring = a.tensor(); x.state = a.tensor();
+  x.p.pos = a.i32();
+  x.p.feature_map = a.i32();
+  x.pos = a.maybe();
+  x.p.layout = a.i32();
+  x.p.flags = (uint32_t)a.i32();
+  const c10::DeviceGuard guard(x.k.device());
+  void* s = a.stream();
+  fill_draft(&x);
+  x.p.H_q = x.p.H_kv;
+  expect(path, at::kInt, {x.p.B, x.p.N}, x.k, "path");
+  expect(n, at::kInt, {x.p.B}, x.k, "n_accepted");
+  x.p.path = ptr<int32_t>(path); x.p.n_accepted = ptr<int32_t>(n);
+  check(released([&] { return E.draft_commit(&x.p, s); }), "rattn_draft_commit");
+  Py_RETURN_NONE;
+}
+
+PyObject* draft_verify(Args a) {
+  rattn_verify_params p;
+  std::memset(&p, 0, sizeof(p));
+  const at::Tensor tokens = a.tensor(), parents = a.tensor(), target = a.tensor(), draft = a.maybe(), u = a.tensor();
+  const c10::DeviceGuard guard(target.device());
+  void* s = a.stream();
+  if (target.dim() != 3) raise(PyExc_ValueError, "target_probs: a three-dimensional tensor is expected");
+  for (int i = 0; i < 3; ++i)
+    if (target.size(i) > INT32_MAX) raise(PyExc_ValueError, "target_probs has the wrong shape");
+  p.B = (int32_t)target.size(0); p.N = (int32_t)target.size(1); p.V = (int32_t)target.size(2);
+  p.dtype = dtype_code(target);
+  expect(draft, target.scalar_type(), target.sizes(), target, "draft_probs");
+  expect(tokens, at::kInt, {p.B, p.N}, target, "tokens");
+  expect(parents, at::kInt, {p.B, p.N}, target, "parents");
+  expect(u, at::kFloat, {p.B, p.N}, target, "u");
+  const at::Tensor path = fresh({p.B, p.N}, at::kInt, target), n = fresh({p.B}, at::kInt, target),
+                   token = fresh({p.B}, at::kInt, target);
+  p.tokens = ptr<int32_t>(tokens); p.parents = ptr<int32_t>(parents);
+  p.target_probs = ptr(target); p.draft_probs = ptr(draft); p.u = ptr<float>(u);
+  p.path = ptr<int32_t>(path); p.n_accepted = ptr<int32_t>(n); p.token = ptr<int32_t>(token);
+  check(released([&] { return E.draft_verify(&p, s); }), "rattn_draft_verify");
+  return three(path, n, token);
+}
+
+// q, k, the axes and the rest of the parameter block; layout is read last of them, so shapes are known there
+struct QkAxes {
+  rattn_qk_params p;
+  rattn_qk_axes x;
+  at::Tensor q, k, at_, q_gain, k_gain;
+};
+void read_axes(Args& a, QkAxes* x) {
+  std::memset(&x->p, 0, sizeof(x->p));
+  std::memset(&x->x, 0, sizeof(x->x));
+  x->at_ = a.tensor();
+  PyObject* sections = PySequence_Fast(a.next(), "sections: a sequence of integers is expected");
+  if (!sections) throw Raised{};
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(sections);
+  bool bad = n < 1 || n > 4;
+  for (Py_ssize_t i = 0; i < n && !bad; ++i) {
+    const long v = PyLong_AsLong(PySequence_Fast_GET_ITEM(sections, i));
+    bad = v < 1 || v > 64;                                     // (an error of the conversion is -1)
+    x->x.sections[i] = (int32_t)v;
+  }
+  Py_DECREF(sections);
+  if (bad) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "sections: one to four numbers of pairs, each at least 1");
+    throw Raised{};
+  }
+  x->x.n_axes = (int32_t)n;
+  x->x.order = a.i32();
+  x->q_gain = a.maybe();
+  x->k_gain = a.maybe();
+  x->p.theta = a.real();
+  x->p.eps = a.real();
+  x->p.layout = a.i32();
+  need_dim(x->q, 4);
+  const int hd = x->p.layout == RATTN_LAYOUT_BTHD ? 2 : 1;
+  rattn_qk_params& p = x->p;
+  p.B = (int32_t)x->q.size(0); p.H_q = (int32_t)x->q.size(hd); p.T = (int32_t)x->q.size(3 - hd); p.d = (int32_t)x->q.size(3);
+  p.q = ptr(x->q);
+  p.dtype = dtype_code(x->q);
+  if (x->k.defined()) {
+    need_dim(x->k, 4);
+    p.H_kv = (int32_t)x->k.size(hd);
+    std::vector<int64_t> sizes = x->q.sizes().vec();
+    sizes[hd] = p.H_kv;
+    expect(x->k, x->q.scalar_type(), sizes, x->q, "k");
+    p.k = ptr(x->k);
+  }
+  expect(x->at_, at::kInt, {x->x.n_axes, p.B, p.T}, x->q, "at");
+  expect(x->q_gain, at::kFloat, {p.d}, x->q, "q_gain");
+  expect(x->k_gain, at::kFloat, {p.d}, x->q, "k_gain");
+  p.q_gain = ptr<float>(x->q_gain); p.k_gain = ptr<float>(x->k_gain);
+  x->x.at = ptr<int32_t>(x->at_);
+}
+
+PyObject* qk_prologue_axes(Args a) {
+  QkAxes x;
+  x.q = a.tensor();
+  x.k = a.maybe();
+  read_axes(a, &x);
+  const bool inplace = a.flag();
+  const c10::DeviceGuard guard(x.q.device());
+  void* s = a.stream();
+  const at::Tensor q_out = inplace ? x.q : like(x.q), k_out = !x.k.defined() || inplace ? x.k : like(x.k);
+  x.p.q_out = ptr(q_out); x.p.k_out = ptr(k_out);
+  check(released([&] { return E.qk_prologue_axes(&x.p, &x.x, s); }), "rattn_qk_prologue_axes");
+  return Py_BuildValue("(NN)", wrap(q_out), wrap(k_out));
+}
+
+PyObject* qk_prologue_axes_backward(Args a) {
+  QkAxes x;
+  x.q = a.tensor();
+  x.k = a.maybe();
+  const at::Tensor dq_out = a.tensor(), dk_out = a.maybe();
+  read_axes(a, &x);
+  const bool gain_grads = a.flag();
+  at::Tensor ws = a.maybe();
+  const c10::DeviceGuard guard(x.q.device());
+  void* s = a.stream();
+  expect(dq_out, x.q.scalar_type(), x.q.sizes(), x.q, "dq_out");
+  if (dk_out.defined() != x.k.defined()) raise(PyExc_ValueError, "dk_out goes with k");
+  if (x.k.defined()) expect(dk_out, x.k.scalar_type(), x.k.sizes(), x.q, "dk_out");
+  const at::Tensor dq = like(x.q), dk = x.k.defined() ? like(x.k) : at::Tensor();
+  at::Tensor dqg, dkg;
+  if (gain_grads) {
+    dqg = fresh({x.q.size(3)}, at::kFloat, x.q);
+    if (x.k.defined()) dkg = fresh({x.q.size(3)}, at::kFloat, x.q);
+    if (!ws.defined()) {
+      const size_t n = E.qk_prologue_workspace_bytes(x.p.B, x.p.H_q, x.p.H_kv, x.p.T, x.p.d);
+      ws = fresh({(int64_t)n}, at::kByte, x.q);
+    }
+  }
+  if (ws.defined() && ws.device() != x.q.device()) raise(PyExc_ValueError, "workspace is on another device");
+  const size_t nbytes = ws.defined() ? (size_t)ws.nbytes() : 0;
+  check(released([&] {
+          return E.qk_prologue_axes_backward(&x.p, &x.x, ptr(dq_out), ptr(dk_out), ptr(dq), ptr(dk), ptr<float>(dqg),
+                                             ptr<float>(dkg), ptr(ws), nbytes, s);
+        }), "rattn_qk_prologue_axes_backward");
+  return Py_BuildValue("(NNNN)", wrap(dq), wrap(dk), wrap(dqg), wrap(dkg));
+}
+
 // bind(error class, addresses of the entry points in the order of `Entry`)
 PyObject* bind(Args a) {
   PyObject* err = a.next();
   Py_INCREF(err);
   Py_XSETREF(g_error, err);
-  void* at[10];
+  void* at[15];
   for (void*& f : at) {
     f = PyLong_AsVoidPtr(a.next());
     if (!f) raise(PyExc_ValueError, "an entry point is missing");
@@ -402,7 +631,8 @@ PyObject* bind(Args a) {
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(forward), METHOD(forward_static), METHOD(forward_ex), METHOD(backward),
                          METHOD(backward_ex), METHOD(decode_step), METHOD(decode_step_ex), METHOD(qk_prologue),
-                         METHOD(qk_prologue_backward), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(qk_prologue_backward), METHOD(qk_prologue_axes), METHOD(qk_prologue_axes_backward),
+                         METHOD(draft_attention), METHOD(draft_commit), METHOD(draft_verify), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

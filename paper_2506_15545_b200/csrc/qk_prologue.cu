@@ -27,6 +27,15 @@ constexpr int QK_CTAS_PER_SM = 3;
 struct Freqs {
   double inv[64];                     // theta^(-2i/d), i < d/2
 };
+// Tokens with a coordinate on each of several axes: pair i turns by the coordinate on its own axis times inv[i] (0 for the
+// pairs that are not rotated).
+struct AxesFreqs : Freqs {
+  unsigned char axis[64];
+  const int* at;                      // [n_axes, B, T]
+  size_t tokens;                      // B T
+};
+template <bool AXES> struct FreqsOf { using Type = Freqs; };
+template <> struct FreqsOf<true> { using Type = AxesFreqs; };
 
 struct QkArgs {
   const void* x[2];                   // q, k
@@ -47,6 +56,19 @@ struct QkArgs {
 };
 
 __device__ int g_qk_status;           // RATTN_ERR_TIMEOUT once a bounded wait has expired
+
+// The angle of pair i for token t of batch entry b, reduced to [-pi, pi] in fp64: an fp32 product would be off by up to
+// 0.01 rad at position 1e5.
+__device__ __forceinline__ float reduced(double ang) {
+  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  return (float)(ang - kTwoPi * rint(ang * (1.0 / kTwoPi)));
+}
+__device__ __forceinline__ float angle(const QkArgs& a, const Freqs& f, int i, int b, int t) {
+  return reduced((double)((a.pos ? (long long)a.pos[b] : a.pos0) + t) * f.inv[i]);
+}
+__device__ __forceinline__ float angle(const QkArgs& a, const AxesFreqs& f, int i, int b, int t) {
+  return reduced((double)f.at[f.axis[i] * f.tokens + (size_t)b * a.T + t] * f.inv[i]);
+}
 
 template <typename T> struct Io;
 template <> struct Io<__nv_bfloat16> {
@@ -95,22 +117,11 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
-// cos and sin of position * inv_freq for this lane's 8 pairs.  The angle is formed and reduced
-// to [-pi, pi] in fp64: an fp32 product would be off by up to 0.01 rad at position 1e5.
-__device__ __forceinline__ void rotation(const Freqs& f, int first_pair, long long position, int rotate,
-                                         float (&c)[8], float (&s)[8]) {
-  constexpr double kTwoPi = 6.283185307179586476925286766559;
+// cos and sin of the angles of this lane's 8 pairs
+template <typename F>
+__device__ __forceinline__ void rotation(const QkArgs& a, const F& f, int first_pair, int b, int t, float (&c)[8], float (&s)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (rotate) {
-      double ang = (double)position * f.inv[first_pair + j];
-      ang -= kTwoPi * rint(ang * (1.0 / kTwoPi));
-      sincosf((float)ang, &s[j], &c[j]);
-    } else {
-      c[j] = 1.f;
-      s[j] = 0.f;
-    }
-  }
+  for (int j = 0; j < 8; ++j) sincosf(angle(a, f, first_pair + j, b, t), &s[j], &c[j]);
 }
 
 __device__ __forceinline__ void load_gain(const float* gain, int lo_first, int half, float (&g_lo)[8],
@@ -223,9 +234,9 @@ __device__ __forceinline__ void where(const QkArgs& a, const Cursor& c, size_t* 
   }
 }
 
-template <typename T, int D, bool BWD, bool BTHD>
+template <typename T, int D, bool BWD, bool BTHD, bool AXES>
 __global__ void __launch_bounds__(QK_THREADS, BWD ? 2 : QK_CTAS_PER_SM)
-qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Freqs f) {
+qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ typename FreqsOf<AXES>::Type f) {
   using R = Ring<T, BWD>;
   constexpr int LPR = D / 16, RPB = QK_THREADS / LPR, ROW = D * (int)sizeof(T), S = R::kStages;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -300,7 +311,6 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Fre
   int tbl_first = 0, tbl_end = 0;                       // the tokens (entry b, position t: number b T + t) in the table
   auto tbl_at = [&](int tok, int pair) { return tok * (D / 2) + (((pair & 7) >> 1) * LPR + (pair >> 3)) * 2 + (pair & 1); };
   auto fill_table = [&](const Cursor& cx, int i) {
-    constexpr double kTwoPi = 6.283185307179586476925286766559;
     const int H = a.H[cx.which];
     // head vectors from the chunk's first on: this CTA's, the tensor's, as many as a full table's tokens have
     const long long mine = (long long)(hi - i) * RPB, all = (long long)a.B * a.T * H - (long long)cx.c * RPB;
@@ -313,11 +323,8 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Fre
       const int tok = e / (D / 2), pair = e % (D / 2);
       int t = cx.t0 + tok, b = cx.b0;
       while (t >= a.T) { t -= a.T; ++b; }
-      const long long position = (a.pos ? (long long)a.pos[b] : a.pos0) + t;
-      double ang = (double)position * f.inv[pair];
-      ang -= kTwoPi * rint(ang * (1.0 / kTwoPi));
       float sn, cs;
-      sincosf((float)ang, &sn, &cs);
+      sincosf(angle(a, f, pair, b, t), &sn, &cs);
       tbl[tbl_at(tok, pair)] = make_float2(cs, sn);
     }
   };
@@ -351,8 +358,8 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Fre
     if (!BTHD) {
       const int rb = ch.b * a.nblk_t + ch.tb;
       if (rb != cur_rb && a.rotate) {
-        const long long p0 = a.pos ? (long long)a.pos[ch.b] : a.pos0;
-        rotation(f, 8 * l, p0 + ch.tb * RPB + row, a.rotate, c, s);
+        // (rows behind the last token have no coordinates to be read)
+        rotation(a, f, 8 * l, ch.b, AXES ? min(ch.tb * RPB + row, a.T - 1) : ch.tb * RPB + row, c, s);
         cur_rb = rb;
       }
     } else if (tabled) {
@@ -472,8 +479,9 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Fre
 // The forward pass for few head vectors (decoding), where latency counts and not bandwidth: a warp per head vector, lane
 // l holding its pairs (i, i + d/2) of PPL consecutive i.  No staging and no barriers: one load, the sines and cosines
 // under it, one store (1 sequence of 32/8 heads: 3.1 -> 2.2 us).
-template <typename T, int D>
-__global__ void __launch_bounds__(QK_THREADS) qk_small_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Freqs f,
+template <typename T, int D, bool AXES>
+__global__ void __launch_bounds__(QK_THREADS) qk_small_kernel(const __grid_constant__ QkArgs a,
+                                                              const __grid_constant__ typename FreqsOf<AXES>::Type f,
                                                               int ctas_per_token) {
   constexpr int PPL = D / 64;
   const int lane = threadIdx.x & 31, i0 = PPL * lane;
@@ -498,17 +506,11 @@ __global__ void __launch_bounds__(QK_THREADS) qk_small_kernel(const __grid_const
     g_hi[j] = gain ? gain[D / 2 + i0 + j] : 1.f;
   }
   float c[PPL], s[PPL];
-  const long long position = (a.pos ? (long long)a.pos[b] : a.pos0) + t;
 #pragma unroll
   for (int j = 0; j < PPL; ++j) {
     c[j] = 1.f;
     s[j] = 0.f;
-    if (a.rotate) {
-      constexpr double kTwoPi = 6.283185307179586476925286766559;
-      double ang = (double)position * f.inv[i0 + j];
-      ang -= kTwoPi * rint(ang * (1.0 / kTwoPi));
-      sincosf((float)ang, &s[j], &c[j]);
-    }
+    if (a.rotate) sincosf(angle(a, f, i0 + j, b, t), &s[j], &c[j]);
   }
 #pragma unroll
   for (int j = 0; j < PPL; ++j) ss += lo[j] * lo[j] + hi[j] * hi[j];
@@ -535,8 +537,8 @@ long long small_limit(const QkArgs& a, int d, int n_sm) {
   return n < QK_SMALL_VECTORS ? n : QK_SMALL_VECTORS;
 }
 
-template <typename T, int D>
-cudaError_t launch_small(const QkArgs& a, const Freqs& f, cudaStream_t s) {
+template <typename T, int D, bool AXES>
+cudaError_t launch_small(const QkArgs& a, const typename FreqsOf<AXES>::Type& f, cudaStream_t s) {
   const long long tokens = (long long)a.B * a.T;
   const int ctas_per_token = (a.H[0] + a.H[1] + QK_THREADS / 32 - 1) / (QK_THREADS / 32);
   KernelTimer kt("qk_prologue", s);
@@ -549,7 +551,7 @@ cudaError_t launch_small(const QkArgs& a, const Freqs& f, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, qk_small_kernel<T, D>, a, f, ctas_per_token);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, qk_small_kernel<T, D, AXES>, a, f, ctas_per_token);
   if (e != cudaSuccess) return e;
   count_launches(1);
   return cudaGetLastError();
@@ -627,7 +629,7 @@ void fill(const rattn_qk_params* p, QkArgs* a, Freqs* f) {
   a->partial = nullptr;
   a->dy[0] = a->dy[1] = nullptr;
   a->y[0] = a->y[1] = nullptr;
-  if (!a->rotate) return;                  // the kernels then read no frequency
+  if (!a->rotate || !f) return;            // the kernels then read no frequency, or others
   // The frequencies depend on theta and d alone, which a model never changes: 64 powers (2.5 us of host time) are
   // formed when a thread meets another pair of them.
   thread_local struct { float theta = 0.f; int d = 0; Freqs f; } known;
@@ -651,10 +653,10 @@ cudaError_t grid_size(const QkArgs& a, int per_sm, int* n_cta) {
   return cudaSuccess;
 }
 
-template <typename T, int D, bool BWD, bool BTHD>
-cudaError_t launch_layout(const QkArgs& a, const Freqs& f, int n_cta, cudaStream_t s) {
+template <typename T, int D, bool BWD, bool BTHD, bool AXES>
+cudaError_t launch_layout(const QkArgs& a, const typename FreqsOf<AXES>::Type& f, int n_cta, cudaStream_t s) {
   const int smem = Ring<T, BWD>::kBytes + a.tbl_tokens * (D / 2) * (int)sizeof(float2);
-  cudaError_t e = allow_smem<qk_prologue_kernel<T, D, BWD, BTHD>>(smem);
+  cudaError_t e = allow_smem<qk_prologue_kernel<T, D, BWD, BTHD, AXES>>(smem);
   if (e != cudaSuccess) return e;
   KernelTimer kt(BWD ? "qk_prologue_bwd" : "qk_prologue", s);
   cudaLaunchConfig_t cfg = {};
@@ -667,28 +669,139 @@ cudaError_t launch_layout(const QkArgs& a, const Freqs& f, int n_cta, cudaStream
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, qk_prologue_kernel<T, D, BWD, BTHD>, a, f);
+  e = cudaLaunchKernelEx(&cfg, qk_prologue_kernel<T, D, BWD, BTHD, AXES>, a, f);
   if (e != cudaSuccess) return e;
   count_launches(1);
   return cudaGetLastError();
 }
 
-template <typename T, int D, bool BWD>
-cudaError_t launch_one(const QkArgs& a, const Freqs& f, int n_cta, cudaStream_t s) {
-  return a.layout == RATTN_LAYOUT_BHTD ? launch_layout<T, D, BWD, false>(a, f, n_cta, s)
-                                       : launch_layout<T, D, BWD, true>(a, f, n_cta, s);
+template <typename T, int D, bool BWD, bool AXES>
+cudaError_t launch_one(const QkArgs& a, const typename FreqsOf<AXES>::Type& f, int n_cta, cudaStream_t s) {
+  return a.layout == RATTN_LAYOUT_BHTD ? launch_layout<T, D, BWD, false, AXES>(a, f, n_cta, s)
+                                       : launch_layout<T, D, BWD, true, AXES>(a, f, n_cta, s);
 }
 
-template <bool BWD>
-cudaError_t launch(const QkArgs& a, const Freqs& f, int d, int dtype, int n_cta, cudaStream_t s) {
+template <bool BWD, bool AXES>
+cudaError_t launch(const QkArgs& a, const typename FreqsOf<AXES>::Type& f, int d, int dtype, int n_cta, cudaStream_t s) {
   if (dtype == RATTN_BF16)
-    return d == 128 ? launch_one<__nv_bfloat16, 128, BWD>(a, f, n_cta, s) : launch_one<__nv_bfloat16, 64, BWD>(a, f, n_cta, s);
-  return d == 128 ? launch_one<float, 128, BWD>(a, f, n_cta, s) : launch_one<float, 64, BWD>(a, f, n_cta, s);
+    return d == 128 ? launch_one<__nv_bfloat16, 128, BWD, AXES>(a, f, n_cta, s) : launch_one<__nv_bfloat16, 64, BWD, AXES>(a, f, n_cta, s);
+  return d == 128 ? launch_one<float, 128, BWD, AXES>(a, f, n_cta, s) : launch_one<float, 64, BWD, AXES>(a, f, n_cta, s);
 }
 
 int fail(cudaError_t e) {
   set_last_cuda_error((int)e);
   return RATTN_ERR_CUDA;
+}
+
+int check_axes(const rattn_qk_params* p, const rattn_qk_axes* x) {
+  if (!x) return RATTN_ERR_NULL_PTR;
+  if (x->n_axes < 1 || x->n_axes > 4 || p->pos0 != 0 || p->pos || !(p->theta > 0.f)) return RATTN_ERR_BAD_ARG;
+  long long pairs = 0;
+  for (int i = 0; i < x->n_axes; ++i) {
+    if (x->sections[i] < 1) return RATTN_ERR_BAD_ARG;
+    pairs += x->sections[i];
+  }
+  if (pairs > p->d / 2) return RATTN_ERR_BAD_ARG;
+  if (x->order < RATTN_AXES_RUNS || x->order > RATTN_AXES_DEALT) return RATTN_ERR_UNSUPPORTED;
+  if (!x->at) return RATTN_ERR_NULL_PTR;
+  if (((uintptr_t)x->at & 3u) != 0) return RATTN_ERR_MISALIGNED;
+  return RATTN_OK;
+}
+
+// Axis and frequency of every pair: host work of 64 powers, formed when a thread meets another assignment than its last.
+void fill_axes(const rattn_qk_params* p, const rattn_qk_axes* x, AxesFreqs* f) {
+  thread_local struct { float theta = 0.f; int d = 0; rattn_qk_axes x = {}; AxesFreqs f; } known;
+  bool same = known.theta == p->theta && known.d == p->d && known.x.n_axes == x->n_axes && known.x.order == x->order;
+  for (int i = 0; same && i < x->n_axes; ++i) same = known.x.sections[i] == x->sections[i];
+  if (!same) {
+    int room[4], next = 0, axis = 0;
+    for (int i = 0; i < x->n_axes; ++i) room[i] = x->sections[i];
+    for (int i = 0; i < 64; ++i) {
+      known.f.inv[i] = 0.0;
+      known.f.axis[i] = 0;
+    }
+    auto put = [&](int to, double exponent) {
+      known.f.axis[next] = (unsigned char)to;
+      known.f.inv[next++] = std::pow((double)p->theta, -exponent);
+    };
+    if (x->order == RATTN_AXES_DEALT) {
+      for (int left = 0; left < 64 * 4; ++left, axis = (axis + 1) % x->n_axes)     // 64 pairs, each within n_axes steps
+        if (room[axis] > 0) {
+          --room[axis];
+          put(axis, 2.0 * next / p->d);
+        }
+    } else {
+      for (; axis < x->n_axes; ++axis)
+        for (int j = 0; j < room[axis]; ++j) put(axis, x->order == RATTN_AXES_OWN ? (double)j / room[axis] : 2.0 * next / p->d);
+    }
+    known.theta = p->theta;
+    known.d = p->d;
+    known.x = *x;
+  }
+  *f = known.f;
+  f->at = x->at;
+  f->tokens = (size_t)p->B * p->T;
+}
+
+template <bool AXES>
+int forward(const rattn_qk_params* p, const QkArgs& a, const typename FreqsOf<AXES>::Type& f, cudaStream_t s) {
+  int n_sm = 0;
+  cudaError_t e = sm_count(&n_sm);
+  if (e != cudaSuccess) return fail(e);
+  if ((long long)p->B * p->T * (p->H_q + p->H_kv) <= small_limit(a, p->d, n_sm)) {
+    if (p->dtype == RATTN_BF16)
+      e = p->d == 128 ? launch_small<__nv_bfloat16, 128, AXES>(a, f, s) : launch_small<__nv_bfloat16, 64, AXES>(a, f, s);
+    else
+      e = p->d == 128 ? launch_small<float, 128, AXES>(a, f, s) : launch_small<float, 64, AXES>(a, f, s);
+    return e == cudaSuccess ? RATTN_OK : fail(e);
+  }
+  int n_cta = 0;
+  e = grid_size(a, QK_CTAS_PER_SM, &n_cta);
+  if (e == cudaSuccess) e = launch<false, AXES>(a, f, p->d, p->dtype, n_cta, s);
+  return e == cudaSuccess ? RATTN_OK : fail(e);
+}
+
+int check_forward(const rattn_qk_params* p) {
+  const int rc = check(p);
+  if (rc != RATTN_OK) return rc;
+  if (!p->q_out || (p->H_kv > 0 && !p->k_out)) return RATTN_ERR_NULL_PTR;
+  if (misaligned16(p->q_out) || misaligned16(p->k_out)) return RATTN_ERR_MISALIGNED;
+  return RATTN_OK;
+}
+
+int check_backward(const rattn_qk_params* p, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_gain,
+                   float* dk_gain, void* workspace, size_t workspace_bytes) {
+  const int rc = check(p);
+  if (rc != RATTN_OK) return rc;
+  if (!dq_out || !dq || (p->H_kv > 0 && (!dk_out || !dk))) return RATTN_ERR_NULL_PTR;
+  if (p->H_kv == 0 && dk_gain) return RATTN_ERR_BAD_ARG;
+  if (misaligned16(dq_out) || misaligned16(dk_out) || misaligned16(dq) || misaligned16(dk) ||
+      misaligned16(dq_gain) || misaligned16(dk_gain))
+    return RATTN_ERR_MISALIGNED;
+  if ((dq_gain || dk_gain) &&
+      (!workspace || workspace_bytes < rattn_qk_prologue_workspace_bytes(p->B, p->H_q, p->H_kv, p->T, p->d) ||
+       ((uintptr_t)workspace & 255u) != 0))
+    return RATTN_ERR_WORKSPACE;
+  return RATTN_OK;
+}
+
+template <bool AXES>
+int backward(const rattn_qk_params* p, QkArgs& a, const typename FreqsOf<AXES>::Type& f, const void* dq_out, const void* dk_out,
+             void* dq, void* dk, float* dq_gain, float* dk_gain, void* workspace, cudaStream_t s) {
+  a.y[0] = dq; a.y[1] = dk;
+  a.dy[0] = dq_out; a.dy[1] = dk_out;
+  if (dq_gain || dk_gain) a.partial = static_cast<float*>(workspace);
+  int n_cta = 0;
+  cudaError_t e = grid_size(a, 2, &n_cta);
+  if (e == cudaSuccess) e = launch<true, AXES>(a, f, p->d, p->dtype, n_cta, s);
+  if (e == cudaSuccess && a.partial != nullptr) {
+    KernelTimer kt("qk_gain_reduce", s);
+    if (p->d == 128) qk_gain_reduce_kernel<128><<<2, 1024, 0, s>>>(a.partial, n_cta, dq_gain, dk_gain);
+    else qk_gain_reduce_kernel<64><<<2, 1024, 0, s>>>(a.partial, n_cta, dq_gain, dk_gain);
+    count_launches(1);
+    e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? RATTN_OK : fail(e);
 }
 
 }  // namespace
@@ -704,62 +817,49 @@ size_t rattn_qk_prologue_workspace_bytes(int B, int H_q, int H_kv, int T, int d)
 }
 
 int rattn_qk_prologue(const rattn_qk_params* p, void* stream) {
-  int rc = check(p);
+  const int rc = check_forward(p);
   if (rc != RATTN_OK) return rc;
-  if (!p->q_out || (p->H_kv > 0 && !p->k_out)) return RATTN_ERR_NULL_PTR;
-  if (misaligned16(p->q_out) || misaligned16(p->k_out)) return RATTN_ERR_MISALIGNED;
   QkArgs a;
   Freqs f;
   fill(p, &a, &f);
   a.y[0] = p->q_out; a.y[1] = p->k_out;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  int n_sm = 0;
-  cudaError_t e = sm_count(&n_sm);
-  if (e != cudaSuccess) return fail(e);
-  if ((long long)p->B * p->T * (p->H_q + p->H_kv) <= small_limit(a, p->d, n_sm)) {
-    if (p->dtype == RATTN_BF16) e = p->d == 128 ? launch_small<__nv_bfloat16, 128>(a, f, s) : launch_small<__nv_bfloat16, 64>(a, f, s);
-    else e = p->d == 128 ? launch_small<float, 128>(a, f, s) : launch_small<float, 64>(a, f, s);
-    return e == cudaSuccess ? RATTN_OK : fail(e);
-  }
-  int n_cta = 0;
-  e = grid_size(a, QK_CTAS_PER_SM, &n_cta);
-  if (e == cudaSuccess) e = launch<false>(a, f, p->d, p->dtype, n_cta, s);
-  return e == cudaSuccess ? RATTN_OK : fail(e);
+  return forward<false>(p, a, f, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int rattn_qk_prologue_axes(const rattn_qk_params* p, const rattn_qk_axes* axes, void* stream) {
+  int rc = check_forward(p);
+  if (rc == RATTN_OK) rc = check_axes(p, axes);
+  if (rc != RATTN_OK) return rc;
+  QkArgs a;
+  AxesFreqs f;
+  fill(p, &a, nullptr);
+  fill_axes(p, axes, &f);
+  a.y[0] = p->q_out; a.y[1] = p->k_out;
+  return forward<true>(p, a, f, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int rattn_qk_prologue_backward(const rattn_qk_params* p, const void* dq_out, const void* dk_out, void* dq, void* dk,
                                float* dq_gain, float* dk_gain, void* workspace, size_t workspace_bytes,
                                void* stream) {
-  int rc = check(p);
+  const int rc = check_backward(p, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace, workspace_bytes);
   if (rc != RATTN_OK) return rc;
-  if (!dq_out || !dq || (p->H_kv > 0 && (!dk_out || !dk))) return RATTN_ERR_NULL_PTR;
-  if (p->H_kv == 0 && dk_gain) return RATTN_ERR_BAD_ARG;
-  if (misaligned16(dq_out) || misaligned16(dk_out) || misaligned16(dq) || misaligned16(dk) ||
-      misaligned16(dq_gain) || misaligned16(dk_gain))
-    return RATTN_ERR_MISALIGNED;
   QkArgs a;
   Freqs f;
   fill(p, &a, &f);
-  a.y[0] = dq; a.y[1] = dk;
-  a.dy[0] = dq_out; a.dy[1] = dk_out;
-  if (dq_gain || dk_gain) {
-    if (!workspace || workspace_bytes < rattn_qk_prologue_workspace_bytes(p->B, p->H_q, p->H_kv, p->T, p->d) ||
-        ((uintptr_t)workspace & 255u) != 0)
-      return RATTN_ERR_WORKSPACE;
-    a.partial = static_cast<float*>(workspace);
-  }
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  int n_cta = 0;
-  cudaError_t e = grid_size(a, 2, &n_cta);
-  if (e == cudaSuccess) e = launch<true>(a, f, p->d, p->dtype, n_cta, s);
-  if (e == cudaSuccess && a.partial != nullptr) {
-    KernelTimer kt("qk_gain_reduce", s);
-    if (p->d == 128) qk_gain_reduce_kernel<128><<<2, 1024, 0, s>>>(a.partial, n_cta, dq_gain, dk_gain);
-    else qk_gain_reduce_kernel<64><<<2, 1024, 0, s>>>(a.partial, n_cta, dq_gain, dk_gain);
-    count_launches(1);
-    e = cudaGetLastError();
-  }
-  return e == cudaSuccess ? RATTN_OK : fail(e);
+  return backward<false>(p, a, f, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int rattn_qk_prologue_axes_backward(const rattn_qk_params* p, const rattn_qk_axes* axes, const void* dq_out,
+                                    const void* dk_out, void* dq, void* dk, float* dq_gain, float* dk_gain,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_backward(p, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace, workspace_bytes);
+  if (rc == RATTN_OK) rc = check_axes(p, axes);
+  if (rc != RATTN_OK) return rc;
+  QkArgs a;
+  AxesFreqs f;
+  fill(p, &a, nullptr);
+  fill_axes(p, axes, &f);
+  return backward<true>(p, a, f, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int rattn_qk_prologue_status(void* stream) {
