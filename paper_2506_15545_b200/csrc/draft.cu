@@ -282,7 +282,8 @@ int rattn_draft_attention(const rattn_draft_params* p, void* stream) {
   if (draft::misaligned(p->q) || draft::misaligned(p->out) || draft::misaligned(p->gamma_swa) ||
       draft::misaligned(p->gamma_rla) || draft::misaligned4(p->parents))
     return RATTN_ERR_MISALIGNED;
-  return draft::result(draft::launch_generic(a, reinterpret_cast<cudaStream_t>(stream)));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return draft::result(draft::tc_applies(a) ? draft::launch_tc(a, s) : draft::launch_generic(a, s));
 }
 
 int rattn_draft_commit(const rattn_draft_params* p, void* stream) {
@@ -298,9 +299,10 @@ int rattn_draft_commit(const rattn_draft_params* p, void* stream) {
 }
 
 int rattn_draft_status(void* stream) {
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = cudaStreamSynchronize(s);           // no kernel of these waits on anything yet
-  return draft::result(e);
+  cudaError_t e = cudaSuccess;
+  const int word = draft::tc_status(reinterpret_cast<cudaStream_t>(stream), &e);
+  if (e != cudaSuccess) return draft::result(e);
+  return word == 0 ? RATTN_OK : RATTN_ERR_TIMEOUT;
 }
 
 }  // extern "C"

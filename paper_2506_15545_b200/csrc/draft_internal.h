@@ -64,6 +64,10 @@ __device__ __forceinline__ void node_path(const int* par, int i, NodeSet* s) {
 
 cudaError_t launch_generic(const DraftArgs& a, cudaStream_t s);
 cudaError_t launch_commit(const DraftArgs& a, cudaStream_t s);
+// The tensor-core kernel and its status word (RATTN_ERR_TIMEOUT once a bounded wait has expired; reading clears it).
+bool tc_applies(const DraftArgs& a);
+cudaError_t launch_tc(const DraftArgs& a, cudaStream_t s);
+int tc_status(cudaStream_t s, cudaError_t* err);
 
 }  // namespace draft
 }  // namespace rattn

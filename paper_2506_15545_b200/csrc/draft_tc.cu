@@ -1,0 +1,902 @@
+// Attention of a tree of drafts for bf16, d = 128 and a positive scale (sm_100a: TMA + tcgen05 + TMEM).
+//
+// The rows of a K/V head are its group's query heads at all nodes, R = group * N of them (node by node, so that neighbouring
+// rows share their keys); a CTA takes up to 128.  It walks the ring's slots and then the tree's nodes in tiles of 64 keys:
+//
+//   4 row warps   (thread = row = TMEM lane) online softmax straight out of TMEM; the weights go back over their scores as a
+//                 bf16 pair, leading part and remainder, and P V runs over both: 16 bits of every weight, no restriction on v
+//   MMA warp      S = Q K^T, O += P V (A operand from TMEM), then the linear branch's products
+//   loader warp   TMA: K and V tiles through a ring of five 16 KB slots
+//   2 helper warps  clear V rows that belong to no token or node (0 * NaN), and find nodes whose values are not finite
+//
+// Masks: a row at depth e does not see the e oldest slots (as intervals of slots, in the tiles that hold some of them) and
+// sees the nodes of its own path (128 bits, from a walk up its parents).
+//
+// Linear branch, O_rla = phi(Q) S + (phi(Q) phi(K_far)^T masked) V_far: phi(Q) replaces Q without its normalisation (which the
+// rows apply at the end) as a bf16 pair, S is split likewise, and three products give 16 bits of both; K_far are the at
+// most 127 tokens that have left some row's window (slots of rank < depth; nodes more than w levels up), gathered into a tile.
+// The window output waits in TMEM meanwhile, normalised: its values are then at most sqrt(128), and 16 bits of fixed point
+// hold them to 1.7e-4 (fp16 would be off by 2^-11 of the larger ones, a quarter of the output's own rounding).  y leaves through
+// shared memory, a warp per row, where gains are read once per row and coalesced.
+//
+// Few heads (B H_kv row tiles below the SMs): a cluster of CTAs shares the tiles of keys and the features of S; the partial
+// outputs (fp32) meet through distributed shared memory, a warp per row.
+//
+// A node with a value that is not finite is cleared in the tile (its zero weight would spread it over all rows) and makes the
+// rows that see it NaN.
+#include "draft_internal.h"
+#include "tc_common.cuh"
+
+namespace rattn {
+namespace draft {
+namespace {
+
+using namespace ptx;
+using namespace tc;
+
+constexpr int FAR = 32;                                      // far keys that are taken at a time
+constexpr int DA_NS = 5, DA_THREADS = 256, DA_CLUSTER_ROWS = 96;
+constexpr int DA_OFF_RING = TILE_BYTES;
+constexpr int DA_OFF_BARS = DA_OFF_RING + DA_NS * HT_BYTES;
+constexpr int DA_SMEM = DA_OFF_BARS + 1024;                  // 115,712 bytes: two CTAs share the SM's 228 KB
+constexpr int DA_OFF_OX = DA_SMEM;                           // cluster: [rows][128] fp32 of the window branch, of the linear one
+constexpr int DA_OFF_STAT = DA_OFF_OX + 2 * DA_CLUSTER_ROWS * 512;
+constexpr int DA_SMEM_CLUSTER = DA_OFF_STAT + 2 * DA_CLUSTER_ROWS * 4;
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float PARK = 32767.f / 11.32f;                     // steps per unit of a normalised row of 128 (at most 11.314)
+
+__device__ int g_draft_status;           // RATTN_ERR_TIMEOUT once a bounded wait has expired
+
+struct Bars {
+  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], pv_done, done, drain;
+  // The (at most three) V tiles that are cleaned: landed, cleaned.  Their landing has barriers of its own, because the
+  // helpers follow these uses of the slots alone and a wait by parity cannot skip a phase.
+  uint64_t landed[3], clean[3];
+  uint32_t tmem_base;
+  int abort;
+  uint32_t bad[kMaxNodes / 32];          // nodes with a value that is not finite
+  signed char par[kMaxNodes];            // -2: no node
+  signed char depth[kMaxNodes];          // -1: no node
+  short far_node[kMaxNodes];             // nodes that some row has more than w levels up
+  int n_far_node;
+};
+static_assert(sizeof(Bars) <= DA_SMEM - DA_OFF_BARS, "control block");
+
+struct TcArgs {
+  DraftArgs d;
+  int row_tiles, rows_per_tile, cluster;
+  float scale_log2;
+  int debug_wait;                        // debug build only, 2: a wait counts as run out
+};
+struct alignas(64) TcMaps {
+  CUtensorMap k_ring, v_ring;            // [B*H_kv, w, 128], box 64 columns x 64 slots
+  UMap k, v;                             // the nodes' tensors, box 64 columns x 64 nodes
+};
+
+__device__ __forceinline__ float wmax(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float wsum(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }   // bits < n
+__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// Order of the loads: K_0, K_1, V_0, K_2, V_1, ..., V_{n-1} -- that of their use.
+__device__ __forceinline__ int use_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
+__device__ __forceinline__ int use_v(int t, int n) { return t < n - 1 ? 2 * t + 2 : 2 * n - 1; }
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+// two floats as a bf16 pair word, and the remainders as another
+__device__ __forceinline__ void split2(float a, float b, uint32_t* hi, uint32_t* lo) {
+  const uint32_t h = pack_bf16(a, b);
+  *hi = h;
+  *lo = pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u));
+}
+// byte offset of 16-byte chunk c (0 .. 15) of row r in a [128 x 128] bf16 tile (two swizzled halves), and in a half tile
+__device__ __forceinline__ uint32_t at_tile(int r, int c) { return (uint32_t)((c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+__device__ __forceinline__ uint32_t at_half(int r, int c) { return (uint32_t)((c >> 3) * HT_HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+// an fp32 row of the cluster's exchange: 32 chunks of 16 bytes, permuted so that lanes on different rows meet different banks
+__device__ __forceinline__ uint32_t at_ox(int r, int c) { return (uint32_t)(r * 512 + ((c ^ (r & 31)) << 4)); }
+
+// What a CTA works on.
+struct Item {
+  int b, hk, z, rank, row0, rows;        // rows row0 .. row0 + rows - 1 of K/V head hk of entry b
+  int pos, held, n_ring, t0, nt;         // slots that hold tokens, their tiles; this CTA's tiles: ring tiles, then node tiles
+};
+__device__ __forceinline__ Item make_item(const TcArgs& a, int rank) {
+  const DraftArgs& d = a.d;
+  Item i;
+  const int item = blockIdx.x / a.cluster, rt = item % a.row_tiles;
+  i.z = item / a.row_tiles;
+  i.b = i.z / d.H_kv;
+  i.hk = i.z - i.b * d.H_kv;
+  i.rank = rank;
+  i.row0 = rt * a.rows_per_tile;
+  i.rows = min(a.rows_per_tile, d.group * d.N - i.row0);
+  i.pos = entry_pos(d, i.b);
+  i.held = min(i.pos, d.w);
+  i.n_ring = (i.held + 63) >> 6;
+  const int all = i.n_ring + ((d.N + 63) >> 6);
+  i.t0 = (int)((long long)all * rank / a.cluster);
+  i.nt = (int)((long long)all * (rank + 1) / a.cluster) - i.t0;
+  return i;
+}
+// V tile T may hold rows that are no tokens, or (nodes) values that are not finite
+__device__ __forceinline__ int first_unclean(const Item& it) { return max(it.t0, it.n_ring - ((it.held & 63) ? 1 : 0)); }
+__device__ __forceinline__ bool needs_cleaning(const Item& it, int T) { return T >= first_unclean(it); }
+
+// the use i of the ring of slots (whole warp)
+__device__ __forceinline__ void load_use(const TcMaps& m, const Item& it, unsigned char* smem, Bars* bars, int i) {
+  const bool is_v = i == 2 * it.nt - 1 || (i > 0 && (i & 1) == 0);
+  const int t = i == 0 ? 0 : i == 2 * it.nt - 1 ? it.nt - 1 : is_v ? (i - 2) >> 1 : (i + 1) >> 1, T = it.t0 + t;
+  const int slot = i % DA_NS;
+  unsigned char* dst = smem + DA_OFF_RING + slot * HT_BYTES;
+  uint64_t* bar = &bars->full[slot];
+  if (is_v && needs_cleaning(it, T)) {
+    mbar_arrive_expect_tx(bar, 0);                           // (the phases of the slot's barrier go on)
+    bar = &bars->landed[T - first_unclean(it)];
+  }
+  mbar_arrive_expect_tx(bar, HT_BYTES);
+  if (T < it.n_ring) load_half_tile(dst, is_v ? &m.v_ring : &m.k_ring, bar, 64 * T, it.z);
+  else load_half_tile(dst, is_v ? &m.v : &m.k, bar, 64 * (T - it.n_ring), it.z);
+}
+
+// S = Q K^T of one tile of 64 keys, D[128 x 64]
+__device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k) { mma_k_kh(d, q, k); }
+// O += (hi + lo) V: A from TMEM, hi in columns 0-31, lo in 32-63
+__device__ __forceinline__ void mma_weights(uint32_t o, uint32_t p, uint32_t v, bool acc, int steps) {
+  constexpr uint32_t idesc = instr_desc(128, 128, 0, 1);
+  const uint64_t v0 = mnmajor_base_h(v);
+#pragma unroll
+  for (int part = 0; part < 2; ++part)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < steps) mma_bf16_ts(o, p + 32 * part + 8 * k, v0 + kstep_mn(k), idesc, (acc || part > 0 || k > 0) ? 1u : 0u);
+}
+
+// ---------------------------------------------------------------------------------------------- window loop, by role
+
+__device__ void window_mma(const Item& it, unsigned char* smem, Bars* bars, uint32_t tS, uint32_t tO) {
+  const uint32_t sQ = smem_u32(smem), sR = sQ + DA_OFF_RING;
+  auto scores = [&](int t) {
+    const int i = use_k(t), slot = i % DA_NS;
+    mma_scores(tS + 64 * (t & 1), sQ, sR + slot * HT_BYTES);
+    mma_commit(&bars->s_full[t & 1]);
+    mma_commit(&bars->free_[slot]);
+  };
+  auto wait_use = [&](int i) { mbar_wait_warp(&bars->full[i % DA_NS], (uint32_t)(i / DA_NS) & 1u, &bars->abort); };
+  for (int t = 0; t < 2 && t < it.nt; ++t) {
+    wait_use(use_k(t));
+    tc_fence_after();
+    scores(t);
+  }
+  for (int t = 0; t < it.nt; ++t) {
+    const int i = use_v(t, it.nt), slot = i % DA_NS;
+    if (needs_cleaning(it, it.t0 + t)) mbar_wait_warp(&bars->clean[it.t0 + t - first_unclean(it)], 0u, &bars->abort);
+    else wait_use(i);
+    if (t + 2 < it.nt) wait_use(use_k(t + 2));
+    mbar_wait_warp(&bars->p_ready[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
+    tc_fence_after();
+    mma_weights(tO, tS + 64 * (t & 1), sR + slot * HT_BYTES, t > 0, 4);
+    mma_commit(&bars->pv_done);
+    mma_commit(&bars->free_[slot]);
+    if (t + 2 < it.nt) scores(t + 2);
+  }
+}
+
+__device__ void window_load(const TcMaps& m, const Item& it, unsigned char* smem, Bars* bars) {
+  for (int i = DA_NS; i < 2 * it.nt; ++i) {
+    mbar_wait_warp(&bars->free_[i % DA_NS], (uint32_t)(i / DA_NS - 1) & 1u, &bars->abort);
+    load_use(m, it, smem, bars, i);
+  }
+}
+
+__device__ void window_clean(const DraftArgs& d, const Item& it, unsigned char* smem, Bars* bars, int cid) {
+  for (int T = first_unclean(it); T < it.t0 + it.nt; ++T) {
+    const int n = T - first_unclean(it), slot = use_v(T - it.t0, it.nt) % DA_NS;
+    mbar_wait(&bars->landed[n], 0u, &bars->abort);
+    unsigned char* tile = smem + DA_OFF_RING + slot * HT_BYTES;
+    if (T < it.n_ring) {
+      for (int c = cid + (it.held & 63) * 16; c < 64 * 16; c += 64) *reinterpret_cast<uint4*>(tile + at_half(c >> 4, c & 15)) = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      const int n0 = 64 * (T - it.n_ring);
+      for (int c = cid; c < 64 * 16; c += 64) {
+        uint4* p = reinterpret_cast<uint4*>(tile + at_half(c >> 4, c & 15));
+        const int j = n0 + (c >> 4);
+        const uint4 x = *p;
+        const bool live = bars->depth[j] >= 0, odd = not_finite(x.x) || not_finite(x.y) || not_finite(x.z) || not_finite(x.w);
+        if (!live || odd) *p = make_uint4(0u, 0u, 0u, 0u);
+        if (live && odd) atomicOr(&bars->bad[j >> 5], 1u << (j & 31));
+      }
+    }
+    fence_proxy_async_smem();
+    mbar_arrive(&bars->clean[n]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------- kernel
+
+template <bool CL>
+__global__ void __launch_bounds__(DA_THREADS, CL ? 1 : 2)
+draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps maps) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Bars* bars = reinterpret_cast<Bars*>(smem + DA_OFF_BARS);
+  const DraftArgs& d = a.d;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = d.group;
+  const int CS = CL ? a.cluster : 1, rank = CL ? (int)(blockIdx.x % CS) : 0;
+  if (tid == 0) {
+    const int rows = min(a.rows_per_tile, G * d.N - (int)(blockIdx.x / CS) % a.row_tiles * a.rows_per_tile);
+    for (int i = 0; i < DA_NS; ++i) {
+      mbar_init(&bars->full[i], 1);
+      mbar_init(&bars->free_[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->s_full[i], 1);
+      mbar_init(&bars->p_ready[i], (uint32_t)((rows + 31) & ~31));      // the warps that have rows
+    }
+    mbar_init(&bars->pv_done, 1);
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&bars->landed[i], 1);
+      mbar_init(&bars->clean[i], 64);
+    }
+    mbar_init(&bars->done, 1);
+    mbar_init(&bars->drain, 1);
+    bars->abort = 0;
+    for (int i = 0; i < kMaxNodes / 32; ++i) bars->bad[i] = 0u;
+    bars->n_far_node = 0;
+    fence_mbar_init();
+  }
+  if (warp == 4) {
+    tmem_alloc(&bars->tmem_base, 256);
+    tmem_relinquish();
+  }
+  if (tid == 160) {
+    prefetch_tensormap(&maps.k_ring);
+    prefetch_tensormap(&maps.v_ring);
+    prefetch_map(&maps.k);
+    prefetch_map(&maps.v);
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");        // the inputs may come from the kernel before
+  const Item it = make_item(a, rank);
+  if (tid < kMaxNodes) {
+    const int p = tid < d.N ? d.parents[(size_t)it.b * d.N + tid] : -2;
+    bars->par[tid] = (signed char)(p == -1 || (p >= 0 && p < tid) ? p : -2);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  // (behind the allocation of TMEM: a kernel that is set up under this one may want some, too)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t tmem = bars->tmem_base, tS = tmem, tO = tmem + 128;
+
+  if (warp == 5) {
+    for (int i = 0; i < DA_NS && i < 2 * it.nt; ++i) load_use(maps, it, smem, bars, i);
+  } else if (warp >= 6) {                                    // depths; the state on its way to L2
+    for (int n = tid - 192; n < kMaxNodes; n += 64) {
+      int e = 0, j = n;
+      for (;;) {
+        const int p = bars->par[j];
+        if (p < 0) { e = p == -1 ? e : -1; break; }
+        j = p;
+        ++e;
+      }
+      bars->depth[n] = (signed char)e;
+    }
+    const char* S = reinterpret_cast<const char*>(d.state + (size_t)it.z * TILE * TILE) + (size_t)rank * (TILE / CS) * 512;
+    for (int i = tid - 192; i < TILE / CS * 4; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(S + i * 128));
+  } else {
+    // Q rows into the swizzled tile (rows beyond the item's are zero): 160 threads, 16 bytes at a time
+    for (int c = tid; c < TILE * 16; c += 160) {
+      const int r = c >> 4, row = it.row0 + r;
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (r < it.rows)
+        x = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(d.q) + node_at(d, it.b, it.hk * G + row % G, d.H_q, row / G))[c & 15];
+      *reinterpret_cast<uint4*>(smem + at_tile(r, c & 15)) = x;
+    }
+    fence_proxy_async_smem();
+  }
+  __syncthreads();
+
+  // the deepest node, in every warp
+  int dmax = 0;
+  for (int n = lane; n < kMaxNodes; n += 32) dmax = max(dmax, (int)bars->depth[n]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) dmax = max(dmax, __shfl_xor_sync(0xffffffffu, dmax, o));
+  const RingAge age(it.pos, d.w);
+
+  // this thread's row (row warps)
+  const int row = it.row0 + tid, node = warp < 4 && tid < it.rows ? row / G : -1;
+  const int e = node >= 0 ? bars->depth[node] : -1;
+  const uint32_t lanes = (uint32_t)((tid & 96) << 16);       // TMEM lane of the row
+  uint32_t near[4] = {0u, 0u, 0u, 0u}, far[4] = {0u, 0u, 0u, 0u};
+  float m_ref = -INFINITY, l = 0.f;
+
+  if (warp < 4) {
+    if (e >= 0) {
+      int dist = 0;
+      for (int j = node; j >= 0; j = bars->par[j], ++dist) {
+        const uint32_t bit = 1u << (j & 31);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if ((j >> 5) == i && dist <= d.w) near[i] |= bit;
+          if ((j >> 5) == i && dist > d.w) far[i] |= bit;
+        }
+      }
+    }
+    if (32 * warp < it.rows) {
+      const int ee = max(e, 0);
+      for (int t = 0; t < it.nt; ++t) {
+        const int T = it.t0 + t;
+        const uint32_t ts = tS + 64 * (t & 1) + lanes;
+        uint64_t keep;
+        bool all;
+        if (T < it.n_ring) {
+          // slot s is kept if s < held and its rank is e or more
+          const int s0 = 64 * T, h = age.head - s0;
+          auto kept = [&](int depth) { return below(it.held - s0) & (~below(h + depth) | (below(h) & ~below(h + depth - d.w))); };
+          all = kept(dmax) == ~0ull;
+          keep = all ? ~0ull : kept(ee);
+        } else {
+          const bool second = T > it.n_ring;
+          keep = second ? (uint64_t)near[3] << 32 | near[2] : (uint64_t)near[1] << 32 | near[0];
+          all = false;
+        }
+        mbar_wait(&bars->s_full[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
+        tc_fence_after();
+        float x[64];
+        tmem_ld32(ts, reinterpret_cast<float(&)[32]>(x[0]));
+        tmem_ld32(ts + 32, reinterpret_cast<float(&)[32]>(x[32]));
+        tmem_wait_ld();
+        if (!all) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (!((uint32_t)keep >> i & 1u)) x[i] = -INFINITY;
+            if (!((uint32_t)(keep >> 32) >> i & 1u)) x[32 + i] = -INFINITY;
+          }
+        }
+        float mx = fmaxf(max32(reinterpret_cast<float(&)[32]>(x[0])), max32(reinterpret_cast<float(&)[32]>(x[32])));
+        mx *= a.scale_log2;                                  // scale > 0
+        // lazy rescale: the reference maximum moves when the row's grew by more than 2^8
+        if (__any_sync(0xffffffffu, mx > m_ref + 8.f || m_ref == -INFINITY)) {
+          const float m_new = fmaxf(m_ref, mx);
+          if (t > 0) {
+            const float f = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
+            mbar_wait(&bars->pv_done, (uint32_t)(t - 1) & 1u, &bars->abort);
+            tc_fence_after();
+            __syncwarp();
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              float o[16];
+              tmem_ld16(tO + lanes + 16 * c, o);
+              tmem_wait_ld();
+              uint32_t ow[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) ow[i] = __float_as_uint(o[i] * f);
+              tmem_st16(tO + lanes + 16 * c, ow);
+            }
+            l *= f;
+          }
+          m_ref = m_new;
+        }
+        const float ms = m_ref == -INFINITY ? 0.f : m_ref;
+        float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+        const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), nm2 = make_float2(-ms, -ms);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t hi[16], lo[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 y = __ffma2_rn(make_float2(x[32 * c + 2 * i], x[32 * c + 2 * i + 1]), sc2, nm2);
+            const float2 p = make_float2(ex2(y.x), ex2(y.y));
+            if (i & 1) sum1 = __fadd2_rn(sum1, p);
+            else sum0 = __fadd2_rn(sum0, p);
+            split2(p.x, p.y, &hi[i], &lo[i]);
+          }
+          tmem_st16(ts + 16 * c, hi);
+          tmem_st16(ts + 32 + 16 * c, lo);
+        }
+        l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&bars->p_ready[t & 1]);
+      }
+      // The last product but one may be under way still (the last scores went out ahead of it), and a wait by parity cannot
+      // skip a phase: one after the other.
+      if (it.nt > 1) mbar_wait(&bars->pv_done, (uint32_t)(it.nt - 2) & 1u, &bars->abort);
+      if (it.nt > 0) mbar_wait(&bars->pv_done, (uint32_t)(it.nt - 1) & 1u, &bars->abort);
+      tc_fence_after();
+      __syncwarp();
+    }
+  } else if (warp == 4) {
+    window_mma(it, smem, bars, tS, tO);
+#ifdef RATTN_DEBUG_KNOBS
+    if (a.debug_wait == 2 && rank == CS - 1) bars->abort = 1;     // as if one of its waits had run out
+#endif
+  } else if (warp == 5) {
+    window_load(maps, it, smem, bars);
+  } else {
+    window_clean(d, it, smem, bars, tid - 192);
+    // nodes that some row has more than w levels up
+    if (dmax > d.w && tid == 192) {
+      int n = 0;
+      for (int j = 0; j < d.N; ++j)
+        if (bars->depth[j] >= 0 && bars->depth[j] < dmax - d.w) bars->far_node[n++] = (short)j;
+      bars->n_far_node = n;
+    }
+  }
+  __syncthreads();                       // the window's products are complete, its slots free, all nodes looked at
+  tc_fence_after();
+
+  // ---- linear branch -----------------------------------------------------------------------------------------------
+  // Slots: 0, 1 the remainders of phi(Q); 2, 3 half of S (64 features), leading parts and remainders; 4 phi(K_far); V_far in 2.
+  const uint32_t sQ = smem_u32(smem), sR = sQ + DA_OFF_RING;
+  unsigned char* slots = smem + DA_OFF_RING;
+  float* stat = reinterpret_cast<float*>(smem + DA_OFF_STAT);
+  const int k0 = 8 * rank / CS, k1 = 8 * (rank + 1) / CS;    // this CTA's steps of 16 features
+  const float* S = d.state + (size_t)it.z * TILE * TILE;
+  const int corner = max(0, min(dmax, d.w) - age.first);     // far slots: ranks first .. first + corner - 1
+  const int n_far = rank == 0 ? corner + bars->n_far_node : 0;
+  const bool row_warp = warp < 4 && 32 * warp < it.rows;
+  float inv_phi = 1.f;                                       // of the row's feature map
+  bool finite = true;                                        // the row's window output
+  uint32_t done_phase = 0;
+
+  // 16 float4 of S per thread (128 threads), then their two halves to slots 2, 3
+  auto load_s = [&](int hh, float4 (&x)[16]) {
+    const int c = tid - 128;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int f = 64 * hh + (c >> 5) + 4 * i;
+      x[i] = f >= 16 * k0 && f < 16 * k1 ? *reinterpret_cast<const float4*>(S + (size_t)f * TILE + (c & 31) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  };
+  auto store_s = [&](const float4 (&x)[16]) {
+    const int c = tid - 128;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      uint2 hi, lo;
+      split2(x[i].x, x[i].y, &hi.x, &lo.x);
+      split2(x[i].z, x[i].w, &hi.y, &lo.y);
+      const uint32_t at = at_half((c >> 5) + 4 * i, (c & 31) >> 1) + (c & 1) * 8;
+      *reinterpret_cast<uint2*>(slots + 2 * HT_BYTES + at) = hi;
+      *reinterpret_cast<uint2*>(slots + 3 * HT_BYTES + at) = lo;
+    }
+    fence_proxy_async_smem();
+  };
+  // products of the features 64 hh .. 64 hh + 63 with this CTA's part of S (MMA warp)
+  auto mma_state = [&](int hh, bool acc) {
+    constexpr uint32_t idesc = instr_desc(128, 128, 0, 1);
+#pragma unroll
+    for (int term = 0; term < 3; ++term) {                   // phi hi S hi, phi hi S lo, phi lo S hi
+      const uint64_t a0 = kmajor_base(term == 2 ? sR : sQ), b0 = mnmajor_base_h(sR + (term == 1 ? 3 : 2) * HT_BYTES);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (4 * hh + k >= k0 && 4 * hh + k < k1) {
+          mma_bf16(tS, a0 + kstep_k(4 * hh + k, HALF_BYTES), b0 + kstep_mn(k), idesc, acc ? 1u : 0u);
+          acc = true;
+        }
+    }
+    return acc;
+  };
+
+  if (row_warp) {
+    // the window output leaves the accumulator
+    const bool seen = ((near[0] | far[0]) & bars->bad[0]) | ((near[1] | far[1]) & bars->bad[1]) | ((near[2] | far[2]) & bars->bad[2]) |
+                      ((near[3] | far[3]) & bars->bad[3]);
+    if (CL) {
+      if (tid < DA_CLUSTER_ROWS) {
+        stat[tid] = m_ref;
+        stat[DA_CLUSTER_ROWS + tid] = seen ? __uint_as_float(0x7fc00000u) : l;
+      }
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        if (it.nt > 0) {
+          tmem_ld32(tO + lanes + 32 * c, o);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<float4*>(smem + DA_OFF_OX + at_ox(tid, 8 * c + i)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      }
+    } else {
+      const float inv = (seen ? __uint_as_float(0x7fc00000u) : 1.f) / l;
+      float ss = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        tmem_ld32(tO + lanes + 32 * c, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) ss += (o[i] * inv) * (o[i] * inv);
+      }
+      const float f = PARK * inv * rsqrtf(ss * (1.f / TILE) + d.eps);
+      finite = ss < INFINITY;                                // (false for NaN: the row is then NaN)
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        tmem_ld32(tO + lanes + 32 * c, o);
+        tmem_wait_ld();
+        uint32_t h[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)                         // the low bits of 1.5 2^23 + n are those of n
+          h[i] = __byte_perm(__float_as_uint(fmaf(o[2 * i], f, 12582912.f)), __float_as_uint(fmaf(o[2 * i + 1], f, 12582912.f)), 0x5410);
+        tmem_st16(tO + lanes + 16 * c, h);
+      }
+      tmem_wait_st();
+    }
+    // phi(Q): leading parts over Q, remainders to slots 0, 1
+    float mq = 0.f, sq = 0.f;
+    if (d.phi == RATTN_PHI_SOFTMAX) {
+      mq = -INFINITY;
+#pragma unroll 4
+      for (int c = 0; c < 16; ++c) {
+        const uint4 u = *reinterpret_cast<const uint4*>(smem + at_tile(tid, c));
+        const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mq = fmaxf(mq, fmaxf(__uint_as_float(w4[i] << 16), __uint_as_float(w4[i] & 0xffff0000u)));
+      }
+      mq *= LOG2E;
+    }
+#pragma unroll 4
+    for (int c = 0; c < 16; ++c) {
+      const uint4 u = *reinterpret_cast<const uint4*>(smem + at_tile(tid, c));
+      const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float p = __uint_as_float(w4[i] << 16), q = __uint_as_float(w4[i] & 0xffff0000u);
+        if (d.phi == RATTN_PHI_SOFTMAX) {
+          p = ex2(p * LOG2E - mq);
+          q = ex2(q * LOG2E - mq);
+          sq += p + q;
+        } else if (d.phi == RATTN_PHI_RELU) {
+          p = fmaxf(p, 0.f);
+          q = fmaxf(q, 0.f);
+        }
+        split2(p, q, &hi[i], &lo[i]);
+      }
+      *reinterpret_cast<uint4*>(smem + at_tile(tid, c)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(slots + at_tile(tid, c)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
+    fence_proxy_async_smem();
+  } else if (warp >= 4) {
+    float4 x[16];
+    load_s(0, x);
+    store_s(x);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+
+  // phi(k) of far keys chunk .. chunk + 31 to slot 4, leading parts to its rows 0 - 31 and remainders to 32 - 63 (a row whose
+  // linear branch is a handful of these shows their rounding: 2^-9 of a weight is as much as the output's own): a warp per
+  // key, lane with 4 features
+  auto far_source = [&](int i, bool is_v) -> const __nv_bfloat16* {
+    if (i < corner) return static_cast<const __nv_bfloat16*>(is_v ? d.v_ring : d.k_ring) + ((size_t)it.z * d.w + age.slot(age.first + i)) * TILE;
+    return static_cast<const __nv_bfloat16*>(is_v ? d.v : d.k) + node_at(d, it.b, it.hk, d.H_kv, bars->far_node[i - corner]);
+  };
+  auto build_k = [&](int chunk, int first_warp, int n_warps) {
+    for (int i = warp - first_warp; i < FAR && chunk + i < n_far; i += n_warps) {
+      const uint2 u = reinterpret_cast<const uint2*>(far_source(chunk + i, false))[lane];
+      float x[4] = {__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
+      if (d.phi == RATTN_PHI_SOFTMAX) {
+        const float m = wmax(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += x[j] = ex2((x[j] - m) * LOG2E);
+        const float inv = 1.f / wsum(s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] *= inv;
+      } else if (d.phi == RATTN_PHI_RELU) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = fmaxf(x[j], 0.f);
+      }
+      uint2 hi, lo;
+      split2(x[0], x[1], &hi.x, &lo.x);
+      split2(x[2], x[3], &hi.y, &lo.y);
+      unsigned char* to = slots + 4 * HT_BYTES + at_half(i, lane >> 1) + (lane & 1) * 8;
+      *reinterpret_cast<uint2*>(to) = hi;
+      *reinterpret_cast<uint2*>(to + FAR * 128) = lo;
+    }
+    fence_proxy_async_smem();
+  };
+  auto steps_of = [&](int chunk) { return (min(FAR, n_far - chunk) + 15) >> 4; };
+  // values of the far keys to slot 2, zero behind the last and for nodes that are not finite
+  auto build_v = [&](int chunk, int first_warp, int n_warps) {
+    for (int i = warp - first_warp; i < 16 * steps_of(chunk); i += n_warps) {
+      uint2 u = make_uint2(0u, 0u);
+      if (chunk + i < n_far) {
+        u = reinterpret_cast<const uint2*>(far_source(chunk + i, true))[lane];
+        if (chunk + i >= corner && (not_finite(u.x) || not_finite(u.y))) u = make_uint2(0u, 0u);
+      }
+      *reinterpret_cast<uint2*>(slots + 2 * HT_BYTES + at_half(i, lane >> 1) + (lane & 1) * 8) = u;
+    }
+    fence_proxy_async_smem();
+  };
+  auto mma_far_scores = [&](int chunk) {                      // phi(Q) phi(K_far)^T: hi hi, lo hi, hi lo
+    const uint32_t idesc = instr_desc(128, 16 * steps_of(chunk), 0, 0);
+#pragma unroll
+    for (int term = 0; term < 3; ++term) {
+      const uint64_t a0 = kmajor_base(term == 1 ? sR : sQ), b0 = kmajor_base_h(sR + 4 * HT_BYTES + (term == 2 ? FAR * 128 : 0));
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        mma_bf16(tO + 64, a0 + kstep_k(k, HALF_BYTES), b0 + kstep_k(k, HT_HALF), idesc, (term > 0 || k > 0) ? 1u : 0u);
+    }
+  };
+
+  bool acc = false;
+  if (warp == 4) {
+    acc = mma_state(0, false);
+    mma_commit(&bars->done);
+  }
+  if (warp >= 4) {
+    float4 x[16];
+    load_s(1, x);
+    mbar_wait(&bars->done, 0u, &bars->abort);
+    store_s(x);
+  } else {
+    build_k(0, 0, 4);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 4) {
+    mma_state(1, acc);
+    if (n_far > 0) mma_far_scores(0);
+    mma_commit(&bars->done);
+  }
+  done_phase = 1;
+  for (int chunk = 0; chunk < n_far; chunk += FAR) {          // (the same for all threads of the CTA)
+    mbar_wait(&bars->done, done_phase & 1u, &bars->abort);
+    __syncwarp();
+    tc_fence_after();
+    ++done_phase;
+    if (row_warp) {
+      // corner keys of rank below e, nodes on the path more than w levels up
+      uint32_t keep = (uint32_t)below(min(corner, max(e, 0) - age.first) - chunk);
+      for (int i = max(corner - chunk, 0); i < FAR && chunk + i < n_far; ++i) {
+        const int j = bars->far_node[chunk + i - corner];
+        const uint32_t word = (j >> 5) == 0 ? far[0] : (j >> 5) == 1 ? far[1] : (j >> 5) == 2 ? far[2] : far[3];
+        if (word >> (j & 31) & 1u) keep |= 1u << i;
+      }
+      float x[32];
+      tmem_ld32(tO + 64 + lanes, x);
+      tmem_wait_ld();
+      uint32_t hi[16], lo[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) split2(keep >> (2 * i) & 1u ? x[2 * i] : 0.f, keep >> (2 * i + 1) & 1u ? x[2 * i + 1] : 0.f, &hi[i], &lo[i]);
+      tmem_st16(tO + 64 + lanes, hi);
+      tmem_st16(tO + 96 + lanes, lo);
+      tmem_wait_st();
+    } else if (warp >= 5) {
+      build_v(chunk, 5, 3);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const bool more = chunk + FAR < n_far;
+    if (more && warp < 4) build_k(chunk + FAR, 0, 4);         // the scores of this chunk have been formed
+    if (warp == 4) mma_weights(tS, tO + 64, sR + 2 * HT_BYTES, true, steps_of(chunk));
+    if (more) {
+      __syncthreads();
+      if (warp == 4) mma_far_scores(chunk + FAR);             // behind the product that reads the weights there
+    }
+    if (warp == 4) mma_commit(&bars->done);
+  }
+  mbar_wait(&bars->done, done_phase & 1u, &bars->abort);
+  __syncwarp();
+  tc_fence_after();
+
+  // ---- Section 3.2: two RMS norms and the sum ------------------------------------------------------------------------
+  if (CL) {
+    if (row_warp) {
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        tmem_ld32(tS + lanes + 32 * c, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<float4*>(smem + DA_OFF_OX + DA_CLUSTER_ROWS * 512 + at_ox(tid, 8 * c + i)) =
+              make_float4(o[4 * i] * inv_phi, o[4 * i + 1] * inv_phi, o[4 * i + 2] * inv_phi, o[4 * i + 3] * inv_phi);
+      }
+      tc_fence_before();
+    }
+    __syncthreads();
+    cluster_arrive();                                        // partial outputs of every CTA are in place
+    cluster_wait();
+    // a wait that ran out in one of the CTAs ends the call for all of them
+    const bool ok = !__any_sync(0xffffffffu, lane < CS && __float_as_uint(ld_cluster(cluster_addr(&bars->abort, lane))) != 0u);
+    for (int r = rank + CS * warp; ok && r < it.rows; r += CS * (DA_THREADS / 32)) {
+      const int n = (it.row0 + r) / G, h = it.hk * G + (it.row0 + r) % G, c0 = 4 * lane;
+      if (bars->depth[n] < 0) continue;
+      float m_r = -INFINITY, l_r = 0.f;
+      if (lane < CS) {
+        m_r = ld_cluster(cluster_addr(stat + r, lane));
+        l_r = ld_cluster(cluster_addr(stat + DA_CLUSTER_ROWS + r, lane));
+      }
+      const float m = wmax(m_r), f = ex2(m_r - (m == -INFINITY ? 0.f : m));
+      const float inv = 1.f / wsum(lane < CS ? f * l_r : 0.f);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+      for (int k = 0; k < CS; ++k) {
+        const float fr = __shfl_sync(0xffffffffu, f, k) * inv;
+        const float4 p = ld_cluster4(cluster_addr(smem + DA_OFF_OX + at_ox(r, lane), k));
+        const float4 q = ld_cluster4(cluster_addr(smem + DA_OFF_OX + DA_CLUSTER_ROWS * 512 + at_ox(r, lane), k));
+        x.x += fr * p.x; x.y += fr * p.y; x.z += fr * p.z; x.w += fr * p.w;
+        y.x += q.x; y.y += q.y; y.z += q.z; y.w += q.w;
+      }
+      const float ss = wsum(x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w), sr = wsum(y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w);
+      const float is = rsqrtf(ss / TILE + d.eps), ir = rsqrtf(sr / TILE + d.eps);
+      const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+      const float4 gs = d.gamma_swa ? *reinterpret_cast<const float4*>(d.gamma_swa + (size_t)h * TILE + c0) : one;
+      const float4 gr = d.gamma_rla ? *reinterpret_cast<const float4*>(d.gamma_rla + (size_t)h * TILE + c0) : one;
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
+          make_uint2(pack_bf16(gs.x * x.x * is + gr.x * y.x * ir, gs.y * x.y * is + gr.y * y.y * ir),
+                     pack_bf16(gs.z * x.z * is + gr.z * y.z * ir, gs.w * x.w * is + gr.w * y.w * ir));
+    }
+  } else if (row_warp && !*(volatile int*)&bars->abort) {
+    float ss = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+      float o[32];
+      tmem_ld32(tS + lanes + 32 * c, o);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) ss += (o[i] * inv_phi) * (o[i] * inv_phi);
+    }
+    const float f = inv_phi * rsqrtf(ss * (1.f / TILE) + d.eps);
+    // the window branch as it was parked, rows of 256 bytes over Q; the linear one, normalised, fp32 rows over slots 0 - 3
+    auto at_row = [&](int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 15)) << 4)); };
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+      float o[32], s16[16];
+      tmem_ld32(tS + lanes + 32 * c, o);
+      tmem_ld16(tO + lanes + 16 * c, s16);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint4*>(smem + at_row(tid, 4 * c + i)) =
+            make_uint4(__float_as_uint(s16[4 * i]), __float_as_uint(s16[4 * i + 1]), __float_as_uint(s16[4 * i + 2]), __float_as_uint(s16[4 * i + 3]));
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<float4*>(slots + at_ox(tid, 8 * c + i)) = make_float4(o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f);
+    }
+    tc_fence_before();
+    __syncwarp();
+    const uint32_t nodes = __ballot_sync(0xffffffffu, e >= 0), odd = __ballot_sync(0xffffffffu, !finite);
+    const int c0 = 4 * lane;
+#pragma unroll 2
+    for (int i = 0; i < 32; ++i) {
+      if (!(nodes >> i & 1u)) continue;
+      const int r = 32 * warp + i, n = (it.row0 + r) / G, h = it.hk * G + (it.row0 + r) % G;
+      const short4 u = *reinterpret_cast<const short4*>(smem + at_row(r, lane >> 1) + (lane & 1) * 8);
+      const float4 y = *reinterpret_cast<const float4*>(slots + at_ox(r, lane));
+      const float unit = odd >> i & 1u ? __uint_as_float(0x7fc00000u) : 1.f / PARK;
+      const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+      const float4 gs = d.gamma_swa ? *reinterpret_cast<const float4*>(d.gamma_swa + (size_t)h * TILE + c0) : one;
+      const float4 gr = d.gamma_rla ? *reinterpret_cast<const float4*>(d.gamma_rla + (size_t)h * TILE + c0) : one;
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
+          make_uint2(pack_bf16(gs.x * ((float)u.x * unit) + gr.x * y.x, gs.y * ((float)u.y * unit) + gr.y * y.y),
+                     pack_bf16(gs.z * ((float)u.z * unit) + gr.z * y.z, gs.w * ((float)u.w * unit) + gr.w * y.w));
+    }
+  }
+  if (*(volatile int*)&bars->abort) {
+    // a wait ran out: what is still in flight gets a bounded time to land before the memory goes away
+    if (warp == 4) {
+      mma_commit(&bars->drain);
+      for (int i = 0; i < kWaitPolls && !mbar_try_wait(&bars->drain, 0u); ++i) {}
+    }
+    if (warp == 5) {
+      const int uses = 2 * it.nt;
+      for (int i = max(0, uses - DA_NS); i < uses; ++i)
+        for (int p = 0; p < kWaitPolls && !mbar_try_wait(&bars->full[i % DA_NS], (uint32_t)(i / DA_NS) & 1u); ++p) {}
+      for (int i = 0; i < it.t0 + it.nt - first_unclean(it); ++i)
+        for (int p = 0; p < kWaitPolls && !mbar_try_wait(&bars->landed[i], 0u); ++p) {}
+    }
+    if (tid == 0) g_draft_status = RATTN_ERR_TIMEOUT;
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 4) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 256);
+  }
+  if (CL) {                                                  // nobody leaves while its outputs are being read
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
+}
+
+template <bool CL>
+cudaError_t launch(const TcArgs& a, const TcMaps& m, int items, cudaStream_t s) {
+  constexpr int smem = CL ? DA_SMEM_CLUSTER : DA_SMEM;
+  cudaError_t e = allow_smem<draft_tc_kernel<CL>>(smem);
+  if (e != cudaSuccess) return e;
+  {
+    KernelTimer kt("draft_attention", s);
+    e = launch_pdl_cluster(draft_tc_kernel<CL>, dim3((unsigned)(items * a.cluster)), dim3(DA_THREADS), smem, s, true, a.cluster, a, m);
+    if (e != cudaSuccess) return e;
+  }
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool tc_applies(const DraftArgs& a) {
+  return a.dtype == RATTN_BF16 && a.d == TILE && a.scale > 0.f && !(a.flags & RATTN_FLAG_FORCE_GENERIC);
+}
+
+cudaError_t launch_tc(const DraftArgs& d, cudaStream_t s) {
+  TcArgs a;
+  TcMaps m;
+  a.d = d;
+  a.scale_log2 = d.scale * LOG2E;
+  a.debug_wait = debug_wait();
+  if (!make_map(&m.k_ring, d.k_ring, (uint64_t)d.w, (uint64_t)d.B * d.H_kv, 64) ||
+      !make_map(&m.v_ring, d.v_ring, (uint64_t)d.w, (uint64_t)d.B * d.H_kv, 64) ||
+      !make_user_map(&m.k, d.k, (uint64_t)d.N, (uint64_t)d.H_kv, (uint64_t)d.B, d.layout, 64) ||
+      !make_user_map(&m.v, d.v, (uint64_t)d.N, (uint64_t)d.H_kv, (uint64_t)d.B, d.layout, 64))
+    return cudaErrorInvalidValue;
+  int n_sm = 0;
+  const cudaError_t e = sm_count(&n_sm);
+  if (e != cudaSuccess) return e;
+  const long long R = (long long)d.group * d.N, heads = (long long)d.B * d.H_kv;
+  const int tiles = ((d.pos_dev || d.pos >= d.w ? d.w : d.pos) + 63) / 64 + (d.N + 63) / 64;
+  // Row tiles of a cluster hold at most 96 rows (what the exchange has room for); a cluster has as many CTAs as still find an
+  // SM each, and no more than there are tiles of keys.
+  const long long rt_c = (R + DA_CLUSTER_ROWS - 1) / DA_CLUSTER_ROWS;
+  int cs = 1;
+  while (cs < 8 && 2 * cs <= tiles && heads * rt_c * 2 * cs <= n_sm) cs *= 2;
+  a.cluster = cs;
+  a.row_tiles = (int)(cs > 1 ? rt_c : (R + TILE - 1) / TILE);
+  a.rows_per_tile = (int)((R + a.row_tiles - 1) / a.row_tiles);
+  a.row_tiles = (int)((R + a.rows_per_tile - 1) / a.rows_per_tile);
+  const long long items = heads * a.row_tiles;
+  return cs > 1 ? launch<true>(a, m, (int)items, s) : launch<false>(a, m, (int)items, s);
+}
+
+int tc_status(cudaStream_t s, cudaError_t* err) {
+  int word = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(&word, g_draft_status, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e == cudaSuccess && word != 0) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbolAsync(g_draft_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  }
+  *err = e;
+  return word;
+}
+
+}  // namespace draft
+}  // namespace rattn

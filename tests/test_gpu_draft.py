@@ -6,7 +6,8 @@ kept.  fp32: a score is a sum of d products of unit-norm rows, off by at most d 
 9e-5 and typically by its square root; the framework's bound for fp32 outputs, 1e-4, holds that.  bf16: the output's own
 rounding, half a step, 2^-8 |y|, and 2^-9 times the size of a branch (a row of unit rms: |y| <= 4 nearly always) over the
 root of the number of terms that the 2^-9 roundings of phi(q), phi(k) and of 16-bit weights average over, for which
-2^-10 absolute is allowed.  State after a commit: fp32 sums of n terms, n 2^-23 of the largest entry."""
+2^-10 absolute is allowed.  (The kernels keep 16 bits of each of these, and the window's output waits in fixed point, off by
+1.7e-4 times its gain of up to 1.4: together a third of that.)  State after a commit: fp32 sums of n terms, n 2^-23 of the largest entry."""
 import math
 
 import numpy as np
@@ -463,3 +464,88 @@ def test_binding_checks_types_shapes_and_devices():
         R.rattn_draft_verify(path, path, p, p.bfloat16(), torch.zeros(1, 3, device="cuda"))
     with pytest.raises(ValueError):
         R.rattn_draft_verify(path, path, p, p[:, :2].contiguous(), torch.zeros(1, 3, device="cuda"))
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,N,w,top,kind,layout", [
+    (1, 8, 2, 11, 1000, 5000, "tree", R.LAYOUT_BHTD),         # clusters of eight CTAs, several tiles of keys each
+    (4, 16, 8, 20, 700, 2100, "padded", R.LAYOUT_BTHD),       # of four
+    (9, 8, 8, 6, 1500, 3000, "chain", R.LAYOUT_BHTD),         # of two, many tiles each
+    (25, 32, 8, 20, 448, 1500, "padded", R.LAYOUT_BTHD),      # a CTA per head, more than run at once
+    (19, 40, 8, 64, 640, 1300, "tree", R.LAYOUT_BHTD),        # 320 rows a head: three row tiles, two waves
+    (20, 8, 8, 100, 576, 600, "chain", R.LAYOUT_BTHD),        # a hundred levels
+])
+def test_attention_of_a_batch(B, Hq, Hkv, N, w, top, kind, layout):
+    """Sizes at which CTAs walk many tiles and share keys in every way, each entry at a position of its own: the oracle on two
+    entries, the portable kernel on all."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    rng = np.random.default_rng(N)
+    d, G = 128, Hq // Hkv
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    unit = lambda x: x / x.square().mean(-1, keepdim=True).sqrt()  # noqa: E731
+    pos = rng.integers(1, top, B)
+    pos[0], pos[-1] = min(w + 5, top), top
+    hist = {b: [unit(rnd(Hkv, int(pos[b]), d)).bfloat16(), rnd(Hkv, int(pos[b]), d).bfloat16()] for b in range(B)}
+    kr, vr = (torch.full((B, Hkv, w, d), math.nan, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    state = torch.zeros(B, Hkv, d, d, device="cuda")
+    for b in range(B):
+        p = int(pos[b])
+        slots = torch.arange(max(0, p - w), p, device="cuda") % w
+        for r, x in zip((kr, vr), hist[b]):
+            r[b][:, slots] = x[:, max(0, p - w):]
+        k, v = (x[:, :max(0, p - w)].double() for x in hist[b])
+        state[b] = (torch.softmax(k, -1).transpose(1, 2) @ v).float()
+    q, k, v = unit(rnd(B, Hq, N, d)).bfloat16(), unit(rnd(B, Hkv, N, d)).bfloat16(), rnd(B, Hkv, N, d).bfloat16()
+    parents = np.stack([tree(N, kind, rng) for _ in range(B)])
+    gs, gr = 1 + 0.1 * rnd(Hq, d), 1 + 0.1 * rnd(Hq, d)
+    lay = (lambda x: x.transpose(1, 2).contiguous()) if layout == R.LAYOUT_BTHD else (lambda x: x)
+    out = []
+    for flags in (0, R.FLAG_FORCE_GENERIC, 0):
+        y = R.rattn_draft_attention(lay(q), lay(k), lay(v), torch.tensor(parents, dtype=torch.int32, device="cuda"), kr, vr, state,
+                                    scale=d ** -0.5, gamma_swa=gs, gamma_rla=gr, out=torch.full_like(lay(q), 7.0), layout=layout,
+                                    flags=flags, pos_dev=torch.tensor(pos, dtype=torch.int32, device="cuda"))
+        out.append(lay(y))
+    torch.cuda.synchronize()
+    assert R.rattn_draft_status() == 0
+    assert torch.equal(out[0], out[2])                            # the same bits again
+    a, b = out[0].float(), out[1].float()
+    assert ((a - b).abs() <= 2 * (2.0 ** -8 * b.abs() + 2.0 ** -10)).all()
+    for i in (0, B - 1):
+        heads = [0, Hq - 1]
+        hk = [h // G for h in heads]
+        ref = D.draft_attention(np64(q[i][heads]), np64(k[i][hk]), np64(v[i][hk]), parents[i], np64(hist[i][0][hk]), np64(hist[i][1][hk]),
+                                w, d ** -0.5, gs=np64(gs[heads]), gr=np64(gr[heads]))
+        check(out[0][i][heads], ref, "bf16", i)
+
+
+@pytest.mark.parametrize("B,Hkv,pos", [(1, 2, 900), (40, 8, 300)])
+def test_a_wait_that_runs_out_is_reported(B, Hkv, pos):
+    """The debug build takes a wait of the attention kernel as run out: the call ends, says so once, writes no row, and the next
+    call on the same buffers is right (clusters of CTAs, of which one gives up, and single ones)."""
+    import ctypes
+
+    from paper_2506_15545_b200 import build
+    L = ctypes.CDLL(build.build(debug=True))
+    vp = ctypes.c_void_p
+    L.rattn_draft_attention.argtypes = [ctypes.POINTER(R.RattnDraftParams), vp]
+    L.rattn_draft_status.argtypes = [vp]
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()  # noqa: E731
+    N, w, d = 6, 256, 128
+    q, k, v, kr, vr = rnd(B, Hkv, N, d), rnd(B, Hkv, N, d), rnd(B, Hkv, N, d), rnd(B, Hkv, w, d), rnd(B, Hkv, w, d)
+    state, out = torch.randn(B, Hkv, d, d, device="cuda", generator=g), torch.full_like(q, 7.0)
+    par = torch.tensor([[-1, 0, 1, 1, 2, 0]] * B, dtype=torch.int32, device="cuda")
+    p = R.RattnDraftParams()
+    for f, t in (("q", q), ("k", k), ("v", v), ("out", out), ("parents", par), ("k_ring", kr), ("v_ring", vr), ("state", state)):
+        setattr(p, f, t.data_ptr())
+    p.B, p.H_q, p.H_kv, p.N, p.d, p.w, p.dtype, p.scale, p.eps, p.pos = B, Hkv, Hkv, N, d, w, R.RATTN_BF16, 0.1, 1e-6, pos
+    stream = vp(torch.cuda.current_stream().cuda_stream)
+    try:
+        L.rattn_debug_withhold_arrival(2)
+        assert L.rattn_draft_attention(ctypes.byref(p), stream) == 0
+        assert L.rattn_draft_status(stream) == -7
+        assert (out == 7.0).all()
+    finally:
+        L.rattn_debug_withhold_arrival(0)
+    assert L.rattn_draft_status(stream) == 0
+    assert L.rattn_draft_attention(ctypes.byref(p), stream) == 0 and L.rattn_draft_status(stream) == 0
+    assert torch.equal(out, R.rattn_draft_attention(q, k, v, par, kr, vr, state, pos, scale=0.1))
