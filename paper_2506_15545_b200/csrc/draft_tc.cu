@@ -48,7 +48,7 @@ constexpr float PARK = 32767.f / 11.32f;                     // steps per unit o
 __device__ int g_draft_status;           // RATTN_ERR_TIMEOUT once a bounded wait has expired
 
 struct Bars {
-  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], pv_done, done, drain;
+  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], q_full, pv_done, done, drain;
   // The (at most three) V tiles that are cleaned: landed, cleaned.  Their landing has barriers of its own, because the
   // helpers follow these uses of the slots alone and a wait by parity cannot skip a phase.
   uint64_t landed[3], clean[3];
@@ -58,14 +58,15 @@ struct Bars {
   signed char par[kMaxNodes];            // -2: no node
   signed char depth[kMaxNodes];          // -1: no node
   short far_node[kMaxNodes];             // nodes that some row has more than w levels up
-  int n_far_node;
+  int n_far_node, deepest;
+  unsigned char odd[TILE];               // rows whose window output is not finite
 };
 static_assert(sizeof(Bars) <= DA_SMEM - DA_OFF_BARS, "control block");
 
 struct TcArgs {
   DraftArgs d;
   int row_tiles, rows_per_tile, cluster;
-  float scale_log2;
+  float scale_log2, inv_group;
   int debug_wait;                        // debug build only, 2: a wait counts as run out
 };
 struct alignas(64) TcMaps {
@@ -119,6 +120,13 @@ __device__ __forceinline__ uint32_t at_tile(int r, int c) { return (uint32_t)((c
 __device__ __forceinline__ uint32_t at_half(int r, int c) { return (uint32_t)((c >> 3) * HT_HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 // an fp32 row of the cluster's exchange: 32 chunks of 16 bytes, permuted so that lanes on different rows meet different banks
 __device__ __forceinline__ uint32_t at_ox(int r, int c) { return (uint32_t)(r * 512 + ((c ^ (r & 31)) << 4)); }
+
+// x / G for 0 <= x < 2^21 without an integer division ((x + 0.5) / G is at least 0.5 / G away from an integer, and two
+// roundings by 2^-24 of it are less)
+__device__ __forceinline__ int small_div(int x, float inv) { return __float2int_rd(((float)x + 0.5f) * inv); }
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, bool live) {   // zero where not live
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
 
 // What a CTA works on.
 struct Item {
@@ -187,6 +195,7 @@ __device__ void window_mma(const Item& it, unsigned char* smem, Bars* bars, uint
     mma_commit(&bars->free_[slot]);
   };
   auto wait_use = [&](int i) { mbar_wait_warp(&bars->full[i % DA_NS], (uint32_t)(i / DA_NS) & 1u, &bars->abort); };
+  mbar_wait_warp(&bars->q_full, 0u, &bars->abort);
   for (int t = 0; t < 2 && t < it.nt; ++t) {
     wait_use(use_k(t));
     tc_fence_after();
@@ -256,6 +265,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       mbar_init(&bars->s_full[i], 1);
       mbar_init(&bars->p_ready[i], (uint32_t)((rows + 31) & ~31));      // the warps that have rows
     }
+    mbar_init(&bars->q_full, 128);
     mbar_init(&bars->pv_done, 1);
     for (int i = 0; i < 3; ++i) {
       mbar_init(&bars->landed[i], 1);
@@ -265,7 +275,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
     for (int i = 0; i < kMaxNodes / 32; ++i) bars->bad[i] = 0u;
-    bars->n_far_node = 0;
+    bars->n_far_node = bars->deepest = 0;
     fence_mbar_init();
   }
   if (warp == 4) {
@@ -294,6 +304,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   if (warp == 5) {
     for (int i = 0; i < DA_NS && i < 2 * it.nt; ++i) load_use(maps, it, smem, bars, i);
   } else if (warp >= 6) {                                    // depths; the state on its way to L2
+    int deepest = 0;
     for (int n = tid - 192; n < kMaxNodes; n += 64) {
       int e = 0, j = n;
       for (;;) {
@@ -303,48 +314,45 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         ++e;
       }
       bars->depth[n] = (signed char)e;
+      deepest = max(deepest, e);
     }
+    deepest = __reduce_max_sync(0xffffffffu, deepest);
+    if (lane == 0) atomicMax(&bars->deepest, deepest);
     const char* S = reinterpret_cast<const char*>(d.state + (size_t)it.z * TILE * TILE) + (size_t)rank * (TILE / CS) * 512;
     for (int i = tid - 192; i < TILE / CS * 4; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(S + i * 128));
-  } else {
-    // Q rows into the swizzled tile (rows beyond the item's are zero): 160 threads, 16 bytes at a time
-    for (int c = tid; c < TILE * 16; c += 160) {
-      const int r = c >> 4, row = it.row0 + r;
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (r < it.rows)
-        x = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(d.q) + node_at(d, it.b, it.hk * G + row % G, d.H_q, row / G))[c & 15];
-      *reinterpret_cast<uint4*>(smem + at_tile(r, c & 15)) = x;
+  } else if (warp < 4) {
+    // Q rows into the swizzled tile (rows beyond the item's are zero), 16 bytes at a time; they are awaited below
+    const int c = tid & 15;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = (tid >> 4) + 8 * i, row = it.row0 + min(r, it.rows - 1), n = small_div(row, a.inv_group);
+      copy16_async(smem_u32(smem + at_tile(r, c)),
+                   static_cast<const __nv_bfloat16*>(d.q) + node_at(d, it.b, it.hk * G + row - n * G, d.H_q, n) + 8 * c, r < it.rows);
     }
-    fence_proxy_async_smem();
   }
   __syncthreads();
 
-  // the deepest node, in every warp
-  int dmax = 0;
-  for (int n = lane; n < kMaxNodes; n += 32) dmax = max(dmax, (int)bars->depth[n]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) dmax = max(dmax, __shfl_xor_sync(0xffffffffu, dmax, o));
+  const int dmax = bars->deepest;
   const RingAge age(it.pos, d.w);
 
   // this thread's row (row warps)
-  const int row = it.row0 + tid, node = warp < 4 && tid < it.rows ? row / G : -1;
+  const int node = warp < 4 && tid < it.rows ? small_div(it.row0 + tid, a.inv_group) : -1;
   const int e = node >= 0 ? bars->depth[node] : -1;
   const uint32_t lanes = (uint32_t)((tid & 96) << 16);       // TMEM lane of the row
-  uint32_t near[4] = {0u, 0u, 0u, 0u}, far[4] = {0u, 0u, 0u, 0u};
+  uint64_t near0 = 0, near1 = 0, far0 = 0, far1 = 0;         // nodes 0 - 63, 64 - 127 of its path, up to w levels up and further
   float m_ref = -INFINITY, l = 0.f;
 
   if (warp < 4) {
     if (e >= 0) {
-      int dist = 0;
-      for (int j = node; j >= 0; j = bars->par[j], ++dist) {
-        const uint32_t bit = 1u << (j & 31);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if ((j >> 5) == i && dist <= d.w) near[i] |= bit;
-          if ((j >> 5) == i && dist > d.w) far[i] |= bit;
-        }
+      for (int j = node; j >= 0; j = bars->par[j]) {
+        const uint64_t bit = 1ull << (j & 63);
+        if (e - bars->depth[j] <= d.w) (j < 64 ? near0 : near1) |= bit;
+        else (j < 64 ? far0 : far1) |= bit;
       }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    fence_proxy_async_smem();
+    mbar_arrive(&bars->q_full);
     if (32 * warp < it.rows) {
       const int ee = max(e, 0);
       for (int t = 0; t < it.nt; ++t) {
@@ -359,8 +367,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
           all = kept(dmax) == ~0ull;
           keep = all ? ~0ull : kept(ee);
         } else {
-          const bool second = T > it.n_ring;
-          keep = second ? (uint64_t)near[3] << 32 | near[2] : (uint64_t)near[1] << 32 | near[0];
+          keep = T > it.n_ring ? near1 : near0;
           all = false;
         }
         mbar_wait(&bars->s_full[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
@@ -450,7 +457,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   tc_fence_after();
 
   // ---- linear branch -----------------------------------------------------------------------------------------------
-  // Slots: 0, 1 the remainders of phi(Q); 2, 3 half of S (64 features), leading parts and remainders; 4 phi(K_far); V_far in 2.
+  // Slots: 0, 1 the remainders of phi(Q); 2, 3 half of S (64 features), leading parts and remainders; 4 phi(K_far), then V_far.
   const uint32_t sQ = smem_u32(smem), sR = sQ + DA_OFF_RING;
   unsigned char* slots = smem + DA_OFF_RING;
   float* stat = reinterpret_cast<float*>(smem + DA_OFF_STAT);
@@ -460,8 +467,6 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   const int n_far = rank == 0 ? corner + bars->n_far_node : 0;
   const bool row_warp = warp < 4 && 32 * warp < it.rows;
   float inv_phi = 1.f;                                       // of the row's feature map
-  bool finite = true;                                        // the row's window output
-  uint32_t done_phase = 0;
 
   // 16 float4 of S per thread (128 threads), then their two halves to slots 2, 3
   auto load_s = [&](int hh, float4 (&x)[16]) {
@@ -503,8 +508,8 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 
   if (row_warp) {
     // the window output leaves the accumulator
-    const bool seen = ((near[0] | far[0]) & bars->bad[0]) | ((near[1] | far[1]) & bars->bad[1]) | ((near[2] | far[2]) & bars->bad[2]) |
-                      ((near[3] | far[3]) & bars->bad[3]);
+    const uint64_t bad0 = (uint64_t)bars->bad[1] << 32 | bars->bad[0], bad1 = (uint64_t)bars->bad[3] << 32 | bars->bad[2];
+    const bool seen = (((near0 | far0) & bad0) | ((near1 | far1) & bad1)) != 0;
     if (CL) {
       if (tid < DA_CLUSTER_ROWS) {
         stat[tid] = m_ref;
@@ -536,7 +541,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         for (int i = 0; i < 32; ++i) ss += (o[i] * inv) * (o[i] * inv);
       }
       const float f = PARK * inv * rsqrtf(ss * (1.f / TILE) + d.eps);
-      finite = ss < INFINITY;                                // (false for NaN: the row is then NaN)
+      bars->odd[tid] = !(ss < INFINITY);                     // (NaN too: the row is then NaN)
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         float o[32];
@@ -554,7 +559,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     float mq = 0.f, sq = 0.f;
     if (d.phi == RATTN_PHI_SOFTMAX) {
       mq = -INFINITY;
-#pragma unroll 4
+#pragma unroll
       for (int c = 0; c < 16; ++c) {
         const uint4 u = *reinterpret_cast<const uint4*>(smem + at_tile(tid, c));
         const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
@@ -586,14 +591,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
     if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
     fence_proxy_async_smem();
-  } else if (warp >= 4) {
-    float4 x[16];
-    load_s(0, x);
-    store_s(x);
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
 
   // phi(k) of far keys chunk .. chunk + 31 to slot 4, leading parts to its rows 0 - 31 and remainders to 32 - 63 (a row whose
   // linear branch is a handful of these shows their rounding: 2^-9 of a weight is as much as the output's own): a warp per
@@ -602,8 +600,9 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     if (i < corner) return static_cast<const __nv_bfloat16*>(is_v ? d.v_ring : d.k_ring) + ((size_t)it.z * d.w + age.slot(age.first + i)) * TILE;
     return static_cast<const __nv_bfloat16*>(is_v ? d.v : d.k) + node_at(d, it.b, it.hk, d.H_kv, bars->far_node[i - corner]);
   };
-  auto build_k = [&](int chunk, int first_warp, int n_warps) {
-    for (int i = warp - first_warp; i < FAR && chunk + i < n_far; i += n_warps) {
+  auto build_k = [&](int chunk) {
+#pragma unroll 4
+    for (int i = warp - 4; i < FAR && chunk + i < n_far; i += 4) {
       const uint2 u = reinterpret_cast<const uint2*>(far_source(chunk + i, false))[lane];
       float x[4] = {__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
       if (d.phi == RATTN_PHI_SOFTMAX) {
@@ -628,17 +627,35 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     fence_proxy_async_smem();
   };
   auto steps_of = [&](int chunk) { return (min(FAR, n_far - chunk) + 15) >> 4; };
-  // values of the far keys to slot 2, zero behind the last and for nodes that are not finite
-  auto build_v = [&](int chunk, int first_warp, int n_warps) {
-    for (int i = warp - first_warp; i < 16 * steps_of(chunk); i += n_warps) {
+  // values of the far keys to slot 4, zero behind the last and for nodes that are not finite
+  auto build_v = [&](int chunk) {
+#pragma unroll 4
+    for (int i = warp - 4; i < 16 * steps_of(chunk); i += 4) {
       uint2 u = make_uint2(0u, 0u);
       if (chunk + i < n_far) {
         u = reinterpret_cast<const uint2*>(far_source(chunk + i, true))[lane];
         if (chunk + i >= corner && (not_finite(u.x) || not_finite(u.y))) u = make_uint2(0u, 0u);
       }
-      *reinterpret_cast<uint2*>(slots + 2 * HT_BYTES + at_half(i, lane >> 1) + (lane & 1) * 8) = u;
+      *reinterpret_cast<uint2*>(slots + 4 * HT_BYTES + at_half(i, lane >> 1) + (lane & 1) * 8) = u;
     }
     fence_proxy_async_smem();
+  };
+  // the scores of the far keys become weights: those of corner keys of rank below e and of nodes on the path more than w levels up
+  auto far_weights = [&](int chunk) {
+    uint32_t keep = (uint32_t)below(min(corner, max(e, 0) - age.first) - chunk);
+    for (int i = max(corner - chunk, 0); i < FAR && chunk + i < n_far; ++i) {
+      const int j = bars->far_node[chunk + i - corner];
+      if ((j < 64 ? far0 : far1) >> (j & 63) & 1u) keep |= 1u << i;
+    }
+    float z[32];
+    tmem_ld32(tO + 64 + lanes, z);
+    tmem_wait_ld();
+    uint32_t hi[16], lo[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) split2(keep >> (2 * i) & 1u ? z[2 * i] : 0.f, keep >> (2 * i + 1) & 1u ? z[2 * i + 1] : 0.f, &hi[i], &lo[i]);
+    tmem_st16(tO + 64 + lanes, hi);
+    tmem_st16(tO + 96 + lanes, lo);
+    tmem_wait_st();
   };
   auto mma_far_scores = [&](int chunk) {                      // phi(Q) phi(K_far)^T: hi hi, lo hi, hi lo
     const uint32_t idesc = instr_desc(128, 16 * steps_of(chunk), 0, 0);
@@ -651,68 +668,70 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
   };
 
+  // A: phi(Q), the first half of S and the first far keys are in place
+  float4 x[16];
+  if (warp >= 4) {
+    load_s(0, x);
+    store_s(x);
+    load_s(1, x);
+    build_k(0);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
   bool acc = false;
   if (warp == 4) {
     acc = mma_state(0, false);
+    if (n_far > 0) mma_far_scores(0);
     mma_commit(&bars->done);
   }
+  mbar_wait(&bars->done, 0u, &bars->abort);
+  __syncwarp();
+  tc_fence_after();
+  // B: the second half of S over the first, the values of the far keys over their keys, the weights over their scores
   if (warp >= 4) {
-    float4 x[16];
-    load_s(1, x);
-    mbar_wait(&bars->done, 0u, &bars->abort);
     store_s(x);
-  } else {
-    build_k(0, 0, 4);
+    if (n_far > 0) build_v(0);
+  } else if (row_warp && n_far > 0) {
+    far_weights(0);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp == 4) {
     mma_state(1, acc);
-    if (n_far > 0) mma_far_scores(0);
+    if (n_far > 0) mma_weights(tS, tO + 64, sR + 4 * HT_BYTES, true, steps_of(0));
     mma_commit(&bars->done);
   }
-  done_phase = 1;
-  for (int chunk = 0; chunk < n_far; chunk += FAR) {          // (the same for all threads of the CTA)
-    mbar_wait(&bars->done, done_phase & 1u, &bars->abort);
-    __syncwarp();
-    tc_fence_after();
-    ++done_phase;
-    if (row_warp) {
-      // corner keys of rank below e, nodes on the path more than w levels up
-      uint32_t keep = (uint32_t)below(min(corner, max(e, 0) - age.first) - chunk);
-      for (int i = max(corner - chunk, 0); i < FAR && chunk + i < n_far; ++i) {
-        const int j = bars->far_node[chunk + i - corner];
-        const uint32_t word = (j >> 5) == 0 ? far[0] : (j >> 5) == 1 ? far[1] : (j >> 5) == 2 ? far[2] : far[3];
-        if (word >> (j & 31) & 1u) keep |= 1u << i;
-      }
-      float x[32];
-      tmem_ld32(tO + 64 + lanes, x);
-      tmem_wait_ld();
-      uint32_t hi[16], lo[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) split2(keep >> (2 * i) & 1u ? x[2 * i] : 0.f, keep >> (2 * i + 1) & 1u ? x[2 * i + 1] : 0.f, &hi[i], &lo[i]);
-      tmem_st16(tO + 64 + lanes, hi);
-      tmem_st16(tO + 96 + lanes, lo);
-      tmem_wait_st();
-    } else if (warp >= 5) {
-      build_v(chunk, 5, 3);
-    }
+  uint32_t done_phase = 1;
+  mbar_wait(&bars->done, 1u, &bars->abort);
+  __syncwarp();
+  tc_fence_after();
+  for (int chunk = FAR; chunk < n_far; chunk += FAR) {       // trees deep enough for more of them (the same for all threads)
+    if (warp >= 4) build_k(chunk);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const bool more = chunk + FAR < n_far;
-    if (more && warp < 4) build_k(chunk + FAR, 0, 4);         // the scores of this chunk have been formed
-    if (warp == 4) mma_weights(tS, tO + 64, sR + 2 * HT_BYTES, true, steps_of(chunk));
-    if (more) {
-      __syncthreads();
-      if (warp == 4) mma_far_scores(chunk + FAR);             // behind the product that reads the weights there
+    if (warp == 4) {
+      mma_far_scores(chunk);
+      mma_commit(&bars->done);
     }
-    if (warp == 4) mma_commit(&bars->done);
+    mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
+    __syncwarp();
+    tc_fence_after();
+    if (warp >= 4) build_v(chunk);
+    else if (row_warp) far_weights(chunk);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 4) {
+      mma_weights(tS, tO + 64, sR + 4 * HT_BYTES, true, steps_of(chunk));
+      mma_commit(&bars->done);
+    }
+    mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
+    __syncwarp();
+    tc_fence_after();
   }
-  mbar_wait(&bars->done, done_phase & 1u, &bars->abort);
-  __syncwarp();
-  tc_fence_after();
 
   // ---- Section 3.2: two RMS norms and the sum ------------------------------------------------------------------------
   if (CL) {
@@ -735,7 +754,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     // a wait that ran out in one of the CTAs ends the call for all of them
     const bool ok = !__any_sync(0xffffffffu, lane < CS && __float_as_uint(ld_cluster(cluster_addr(&bars->abort, lane))) != 0u);
     for (int r = rank + CS * warp; ok && r < it.rows; r += CS * (DA_THREADS / 32)) {
-      const int n = (it.row0 + r) / G, h = it.hk * G + (it.row0 + r) % G, c0 = 4 * lane;
+      const int n = small_div(it.row0 + r, a.inv_group), h = it.hk * G + it.row0 + r - n * G, c0 = 4 * lane;
       if (bars->depth[n] < 0) continue;
       float m_r = -INFINITY, l_r = 0.f;
       if (lane < CS) {
@@ -745,13 +764,20 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       const float m = wmax(m_r), f = ex2(m_r - (m == -INFINITY ? 0.f : m));
       const float inv = 1.f / wsum(lane < CS ? f * l_r : 0.f);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-      for (int k = 0; k < CS; ++k) {
-        const float fr = __shfl_sync(0xffffffffu, f, k) * inv;
-        const float4 p = ld_cluster4(cluster_addr(smem + DA_OFF_OX + at_ox(r, lane), k));
-        const float4 q = ld_cluster4(cluster_addr(smem + DA_OFF_OX + DA_CLUSTER_ROWS * 512 + at_ox(r, lane), k));
-        x.x += fr * p.x; x.y += fr * p.y; x.z += fr * p.z; x.w += fr * p.w;
-        y.x += q.x; y.y += q.y; y.z += q.z; y.w += q.w;
-      }
+      float4 p[8], q[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < CS) {
+          p[k] = ld_cluster4(cluster_addr(smem + DA_OFF_OX + at_ox(r, lane), k));
+          q[k] = ld_cluster4(cluster_addr(smem + DA_OFF_OX + DA_CLUSTER_ROWS * 512 + at_ox(r, lane), k));
+        }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < CS) {
+          const float fr = __shfl_sync(0xffffffffu, f, k) * inv;
+          x.x += fr * p[k].x; x.y += fr * p[k].y; x.z += fr * p[k].z; x.w += fr * p[k].w;
+          y.x += q[k].x; y.y += q[k].y; y.z += q[k].z; y.w += q[k].w;
+        }
       const float ss = wsum(x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w), sr = wsum(y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w);
       const float is = rsqrtf(ss / TILE + d.eps), ir = rsqrtf(sr / TILE + d.eps);
       const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
@@ -761,7 +787,9 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
           make_uint2(pack_bf16(gs.x * x.x * is + gr.x * y.x * ir, gs.y * x.y * is + gr.y * y.y * ir),
                      pack_bf16(gs.z * x.z * is + gr.z * y.z * ir, gs.w * x.w * is + gr.w * y.w * ir));
     }
-  } else if (row_warp && !*(volatile int*)&bars->abort) {
+  } else {
+   auto at_row = [&](int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 15)) << 4)); };
+   if (row_warp) {
     float ss = 0.f;
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
@@ -773,7 +801,6 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
     const float f = inv_phi * rsqrtf(ss * (1.f / TILE) + d.eps);
     // the window branch as it was parked, rows of 256 bytes over Q; the linear one, normalised, fp32 rows over slots 0 - 3
-    auto at_row = [&](int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 15)) << 4)); };
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
       float o[32], s16[16];
@@ -789,23 +816,31 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         *reinterpret_cast<float4*>(slots + at_ox(tid, 8 * c + i)) = make_float4(o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f);
     }
     tc_fence_before();
-    __syncwarp();
-    const uint32_t nodes = __ballot_sync(0xffffffffu, e >= 0), odd = __ballot_sync(0xffffffffu, !finite);
-    const int c0 = 4 * lane;
-#pragma unroll 2
-    for (int i = 0; i < 32; ++i) {
-      if (!(nodes >> i & 1u)) continue;
-      const int r = 32 * warp + i, n = (it.row0 + r) / G, h = it.hk * G + (it.row0 + r) % G;
-      const short4 u = *reinterpret_cast<const short4*>(smem + at_row(r, lane >> 1) + (lane & 1) * 8);
-      const float4 y = *reinterpret_cast<const float4*>(slots + at_ox(r, lane));
-      const float unit = odd >> i & 1u ? __uint_as_float(0x7fc00000u) : 1.f / PARK;
-      const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+   }
+   __syncthreads();
+   if (!*(volatile int*)&bars->abort) {
+    // Head by head, so that its gains are read once; a warp takes every eighth of a head's rows, which are G apart.
+    const int c0 = 4 * lane, n0 = small_div(it.row0, a.inv_group), g0 = it.row0 - n0 * G;
+    const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+    for (int i = 0; i < G && i < it.rows; ++i) {             // rows i, i + G, ..: head g of nodes n, n + 1, ..
+      const int wrap = g0 + i >= G, g = g0 + i - (wrap ? G : 0), h = it.hk * G + g;
       const float4 gs = d.gamma_swa ? *reinterpret_cast<const float4*>(d.gamma_swa + (size_t)h * TILE + c0) : one;
       const float4 gr = d.gamma_rla ? *reinterpret_cast<const float4*>(d.gamma_rla + (size_t)h * TILE + c0) : one;
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
-          make_uint2(pack_bf16(gs.x * ((float)u.x * unit) + gr.x * y.x, gs.y * ((float)u.y * unit) + gr.y * y.y),
-                     pack_bf16(gs.z * ((float)u.z * unit) + gr.z * y.z, gs.w * ((float)u.w * unit) + gr.w * y.w));
+      // (the first row of warp `warp` among them; heads in turn start with another warp, so that short ones are shared out)
+      const int k0 = (warp - i) & 7;
+#pragma unroll 2
+      for (int k = k0; i + G * k < it.rows; k += DA_THREADS / 32) {
+        const int r = i + G * k, n = n0 + wrap + k;
+        if (bars->depth[n] < 0) continue;
+        const short4 u = *reinterpret_cast<const short4*>(smem + at_row(r, lane >> 1) + (lane & 1) * 8);
+        const float4 y = *reinterpret_cast<const float4*>(slots + at_ox(r, lane));
+        const float unit = bars->odd[r] ? __uint_as_float(0x7fc00000u) : 1.f / PARK;
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
+            make_uint2(pack_bf16(gs.x * ((float)u.x * unit) + gr.x * y.x, gs.y * ((float)u.y * unit) + gr.y * y.y),
+                       pack_bf16(gs.z * ((float)u.z * unit) + gr.z * y.z, gs.w * ((float)u.w * unit) + gr.w * y.w));
+      }
     }
+   }
   }
   if (*(volatile int*)&bars->abort) {
     // a wait ran out: what is still in flight gets a bounded time to land before the memory goes away
@@ -853,7 +888,7 @@ cudaError_t launch(const TcArgs& a, const TcMaps& m, int items, cudaStream_t s) 
 }  // namespace
 
 bool tc_applies(const DraftArgs& a) {
-  return a.dtype == RATTN_BF16 && a.d == TILE && a.scale > 0.f && !(a.flags & RATTN_FLAG_FORCE_GENERIC);
+  return a.dtype == RATTN_BF16 && a.d == TILE && a.scale > 0.f && a.group <= 4096 && !(a.flags & RATTN_FLAG_FORCE_GENERIC);
 }
 
 cudaError_t launch_tc(const DraftArgs& d, cudaStream_t s) {
@@ -861,6 +896,7 @@ cudaError_t launch_tc(const DraftArgs& d, cudaStream_t s) {
   TcMaps m;
   a.d = d;
   a.scale_log2 = d.scale * LOG2E;
+  a.inv_group = 1.f / (float)d.group;
   a.debug_wait = debug_wait();
   if (!make_map(&m.k_ring, d.k_ring, (uint64_t)d.w, (uint64_t)d.B * d.H_kv, 64) ||
       !make_map(&m.v_ring, d.v_ring, (uint64_t)d.w, (uint64_t)d.B * d.H_kv, 64) ||
