@@ -48,7 +48,7 @@ constexpr float PARK = 32767.f / 11.32f;                     // steps per unit o
 __device__ int g_draft_status;           // RATTN_ERR_TIMEOUT once a bounded wait has expired
 
 struct Bars {
-  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], q_full, pv_done, done, drain;
+  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], q_full, pv_done, scored, o_full, done, drain;
   // The (at most three) V tiles that are cleaned: landed, cleaned.  Their landing has barriers of its own, because the
   // helpers follow these uses of the slots alone and a wait by parity cannot skip a phase.
   uint64_t landed[3], clean[3];
@@ -91,6 +91,8 @@ __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) ==
 __device__ __forceinline__ int use_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int use_v(int t, int n) { return t < n - 1 ? 2 * t + 2 : 2 * n - 1; }
 
+// barrier among n threads (id)
+__device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank) {
@@ -201,6 +203,7 @@ __device__ void window_mma(const Item& it, unsigned char* smem, Bars* bars, uint
     tc_fence_after();
     scores(t);
   }
+  if (it.nt <= 2) mma_commit(&bars->scored);                 // the last scores have gone out
   for (int t = 0; t < it.nt; ++t) {
     const int i = use_v(t, it.nt), slot = i % DA_NS;
     if (needs_cleaning(it, it.t0 + t)) mbar_wait_warp(&bars->clean[it.t0 + t - first_unclean(it)], 0u, &bars->abort);
@@ -209,9 +212,10 @@ __device__ void window_mma(const Item& it, unsigned char* smem, Bars* bars, uint
     mbar_wait_warp(&bars->p_ready[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
     tc_fence_after();
     mma_weights(tO, tS + 64 * (t & 1), sR + slot * HT_BYTES, t > 0, 4);
-    mma_commit(&bars->pv_done);
+    mma_commit(t + 1 < it.nt ? &bars->pv_done : &bars->o_full);
     mma_commit(&bars->free_[slot]);
     if (t + 2 < it.nt) scores(t + 2);
+    if (t + 3 == it.nt) mma_commit(&bars->scored);
   }
 }
 
@@ -271,6 +275,8 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       mbar_init(&bars->landed[i], 1);
       mbar_init(&bars->clean[i], 64);
     }
+    mbar_init(&bars->scored, 1);
+    mbar_init(&bars->o_full, 1);
     mbar_init(&bars->done, 1);
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
@@ -288,22 +294,23 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     prefetch_map(&maps.k);
     prefetch_map(&maps.v);
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");        // the inputs may come from the kernel before
-  const Item it = make_item(a, rank);
-  if (tid < kMaxNodes) {
-    const int p = tid < d.N ? d.parents[(size_t)it.b * d.N + tid] : -2;
-    bars->par[tid] = (signed char)(p == -1 || (p >= 0 && p < tid) ? p : -2);
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   // (behind the allocation of TMEM: a kernel that is set up under this one may want some, too)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = bars->tmem_base, tS = tmem, tO = tmem + 128;
+  asm volatile("griddepcontrol.wait;" ::: "memory");        // the inputs may come from the kernel before
+  const Item it = make_item(a, rank);
 
   if (warp == 5) {
     for (int i = 0; i < DA_NS && i < 2 * it.nt; ++i) load_use(maps, it, smem, bars, i);
-  } else if (warp >= 6) {                                    // depths; the state on its way to L2
+  } else if (warp >= 6) {                                    // the tree; the state on its way to L2
+    for (int n = tid - 192; n < kMaxNodes; n += 64) {
+      const int p = n < d.N ? d.parents[(size_t)it.b * d.N + n] : -2;
+      bars->par[n] = (signed char)(p == -1 || (p >= 0 && p < n) ? p : -2);
+    }
+    named_sync(1, 64);
     int deepest = 0;
     for (int n = tid - 192; n < kMaxNodes; n += 64) {
       int e = 0, j = n;
@@ -323,11 +330,12 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   } else if (warp < 4) {
     // Q rows into the swizzled tile (rows beyond the item's are zero), 16 bytes at a time; they are awaited below
     const int c = tid & 15;
+    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(d.q) + node_at(d, it.b, it.hk * G, d.H_q, 0) + 8 * c;
+    const size_t head = d.layout == RATTN_LAYOUT_BHTD ? (size_t)d.N * TILE : TILE, step = d.layout == RATTN_LAYOUT_BHTD ? TILE : (size_t)d.H_q * TILE;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int r = (tid >> 4) + 8 * i, row = it.row0 + min(r, it.rows - 1), n = small_div(row, a.inv_group);
-      copy16_async(smem_u32(smem + at_tile(r, c)),
-                   static_cast<const __nv_bfloat16*>(d.q) + node_at(d, it.b, it.hk * G + row - n * G, d.H_q, n) + 8 * c, r < it.rows);
+      copy16_async(smem_u32(smem + at_tile(r, c)), q + (row - n * G) * head + n * step, r < it.rows);
     }
   }
   __syncthreads();
@@ -341,14 +349,96 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   const uint32_t lanes = (uint32_t)((tid & 96) << 16);       // TMEM lane of the row
   uint64_t near0 = 0, near1 = 0, far0 = 0, far1 = 0;         // nodes 0 - 63, 64 - 127 of its path, up to w levels up and further
   float m_ref = -INFINITY, l = 0.f;
+  float inv_phi = 1.f;                                       // of the row's feature map
+  // the slots behind the window's last use, oldest first: 0 - 2 are free once the last scores have been formed
+  auto spare_slot = [&](int i) { return (2 * it.nt + i) % DA_NS; };
+  auto spare = [&](int i) { return smem + DA_OFF_RING + spare_slot(i) * HT_BYTES; };
+  const int corner = max(0, min(dmax, d.w) - age.first);     // far slots: ranks first .. first + corner - 1
+
+  // ---- pieces of the linear branch.  Spare slots: 0, 1 the remainders of phi(Q); 2 phi(K_far), then V_far; 3, 4 half of S (64
+  // features), leading parts and remainders.
+  const uint32_t sQ = smem_u32(smem);
+  const int k0 = 8 * rank / CS, k1 = 8 * (rank + 1) / CS;    // this CTA's steps of 16 features
+  const float* S = d.state + (size_t)it.z * TILE * TILE;
+  float4 x_s[16];
+  // 16 float4 of S per thread (128 threads), then their two halves to the last two spare slots
+  auto load_s = [&](int hh, float4 (&x)[16]) {
+    const int c = tid - 128;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int f = 64 * hh + (c >> 5) + 4 * i;
+      x[i] = f >= 16 * k0 && f < 16 * k1 ? *reinterpret_cast<const float4*>(S + (size_t)f * TILE + (c & 31) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  };
+  auto store_s = [&](const float4 (&x)[16]) {
+    const int c = tid - 128;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      uint2 hi, lo;
+      split2(x[i].x, x[i].y, &hi.x, &lo.x);
+      split2(x[i].z, x[i].w, &hi.y, &lo.y);
+      const uint32_t at = at_half((c >> 5) + 4 * i, (c & 31) >> 1) + (c & 1) * 8;
+      *reinterpret_cast<uint2*>(spare(3) + at) = hi;
+      *reinterpret_cast<uint2*>(spare(4) + at) = lo;
+    }
+    fence_proxy_async_smem();
+  };
+  // products of the features 64 hh .. 64 hh + 63 with this CTA's part of S (MMA warp)
+  auto mma_state = [&](int hh, bool acc) {
+    constexpr uint32_t idesc = instr_desc(128, 128, 0, 1);
+#pragma unroll
+    for (int term = 0; term < 3; ++term) {                   // phi hi S hi, phi hi S lo, phi lo S hi
+      const uint64_t a0 = kmajor_base(term == 2 ? smem_u32(spare(hh)) : sQ + hh * HALF_BYTES), b0 = mnmajor_base_h(smem_u32(spare(term == 1 ? 4 : 3)));
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (4 * hh + k >= k0 && 4 * hh + k < k1) {
+          mma_bf16(tS, a0 + kstep_k(k, HALF_BYTES), b0 + kstep_mn(k), idesc, acc ? 1u : 0u);
+          acc = true;
+        }
+    }
+    return acc;
+  };
+
+  // phi(k) of far keys chunk .. chunk + 31 to the third spare slot, leading parts to its rows 0 - 31 and remainders to 32 - 63 (a row whose
+  // linear branch is a handful of these shows their rounding: 2^-9 of a weight is as much as the output's own): a warp per
+  // key, lane with 4 features
+  auto far_source = [&](int i, bool is_v) -> const __nv_bfloat16* {
+    if (i < corner) return static_cast<const __nv_bfloat16*>(is_v ? d.v_ring : d.k_ring) + ((size_t)it.z * d.w + age.slot(age.first + i)) * TILE;
+    return static_cast<const __nv_bfloat16*>(is_v ? d.v : d.k) + node_at(d, it.b, it.hk, d.H_kv, bars->far_node[i - corner]);
+  };
+  auto build_k = [&](int chunk, int n_far, int first_warp, int n_warps) {
+#pragma unroll 2
+    for (int i = warp - first_warp; i < FAR && chunk + i < n_far; i += n_warps) {
+      const uint2 u = reinterpret_cast<const uint2*>(far_source(chunk + i, false))[lane];
+      float x[4] = {__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
+      if (d.phi == RATTN_PHI_SOFTMAX) {
+        const float m = wmax(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += x[j] = ex2((x[j] - m) * LOG2E);
+        const float inv = 1.f / wsum(s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] *= inv;
+      } else if (d.phi == RATTN_PHI_RELU) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = fmaxf(x[j], 0.f);
+      }
+      uint2 hi, lo;
+      split2(x[0], x[1], &hi.x, &lo.x);
+      split2(x[2], x[3], &hi.y, &lo.y);
+      unsigned char* to = spare(2) + at_half(i, lane >> 1) + (lane & 1) * 8;
+      *reinterpret_cast<uint2*>(to) = hi;
+      *reinterpret_cast<uint2*>(to + FAR * 128) = lo;
+    }
+    fence_proxy_async_smem();
+  };
 
   if (warp < 4) {
     if (e >= 0) {
-      for (int j = node; j >= 0; j = bars->par[j]) {
-        const uint64_t bit = 1ull << (j & 63);
-        if (e - bars->depth[j] <= d.w) (j < 64 ? near0 : near1) |= bit;
-        else (j < 64 ? far0 : far1) |= bit;
-      }
+      for (int j = node, up = min(e, d.w); up >= 0; j = bars->par[j], --up) (j < 64 ? near0 : near1) |= 1ull << (j & 63);
+      if (e > d.w)
+        for (int j = node, up = 0; j >= 0; j = bars->par[j], ++up)
+          if (up > d.w) (j < 64 ? far0 : far1) |= 1ull << (j & 63);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     fence_proxy_async_smem();
@@ -429,10 +519,53 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         tc_fence_before();
         mbar_arrive(&bars->p_ready[t & 1]);
       }
-      // The last product but one may be under way still (the last scores went out ahead of it), and a wait by parity cannot
-      // skip a phase: one after the other.
-      if (it.nt > 1) mbar_wait(&bars->pv_done, (uint32_t)(it.nt - 2) & 1u, &bars->abort);
-      if (it.nt > 0) mbar_wait(&bars->pv_done, (uint32_t)(it.nt - 1) & 1u, &bars->abort);
+      mbar_wait(&bars->q_full, 0u, &bars->abort);
+      // phi(Q), while the last products run: every score has been formed and every slot but those of the last two V tiles is
+        // free.  Leading parts go over Q, remainders to the next two slots.
+      // (Loops that run once per row stay rolled: unrolled, they take as long as their instructions take to arrive.)
+      float mq = 0.f, sq = 0.f;
+      const unsigned char* q_row = smem + tid * 128;
+      const int sw = tid & 7;
+      if (d.phi == RATTN_PHI_SOFTMAX) {
+        mq = -INFINITY;
+#pragma unroll 2
+        for (int c = 0; c < 16; ++c) {
+          const uint4 u = *reinterpret_cast<const uint4*>(q_row + (c >> 3) * HALF_BYTES + (((c & 7) ^ sw) << 4));
+          const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mq = fmaxf(mq, fmaxf(__uint_as_float(w4[i] << 16), __uint_as_float(w4[i] & 0xffff0000u)));
+        }
+        mq *= LOG2E;
+      }
+      unsigned char* lo_row = spare(0) + tid * 128;
+      const ptrdiff_t lo_step = spare(1) - spare(0);
+#pragma unroll 2
+      for (int c = 0; c < 16; ++c) {
+        const int at = ((c & 7) ^ sw) << 4;
+        uint4* p16 = reinterpret_cast<uint4*>(smem + tid * 128 + (c >> 3) * HALF_BYTES + at);
+        const uint4 u = *p16;
+        const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float p = __uint_as_float(w4[i] << 16), q = __uint_as_float(w4[i] & 0xffff0000u);
+          if (d.phi == RATTN_PHI_SOFTMAX) {
+            p = ex2(p * LOG2E - mq);
+            q = ex2(q * LOG2E - mq);
+            sq += p + q;
+          } else if (d.phi == RATTN_PHI_RELU) {
+            p = fmaxf(p, 0.f);
+            q = fmaxf(q, 0.f);
+          }
+          split2(p, q, &hi[i], &lo[i]);
+        }
+        *p16 = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(lo_row + (c >> 3) * lo_step + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+      if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
+      fence_proxy_async_smem();
+      // (a barrier of its own: by now pv_done may be one or two phases on)
+      if (it.nt > 0) mbar_wait(&bars->o_full, 0u, &bars->abort);
       tc_fence_after();
       __syncwarp();
     }
@@ -443,69 +576,80 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 #endif
   } else if (warp == 5) {
     window_load(maps, it, smem, bars);
+    load_s(0, x_s);
   } else {
     window_clean(d, it, smem, bars, tid - 192);
-    // nodes that some row has more than w levels up
+    // nodes that some row has more than w levels up; the far keys, as soon as there is room for them
     if (dmax > d.w && tid == 192) {
       int n = 0;
       for (int j = 0; j < d.N; ++j)
         if (bars->depth[j] >= 0 && bars->depth[j] < dmax - d.w) bars->far_node[n++] = (short)j;
       bars->n_far_node = n;
     }
+    named_sync(1, 64);
+    mbar_wait(&bars->scored, 0u, &bars->abort);
+    __syncwarp();
+    if (rank == 0) build_k(0, corner + bars->n_far_node, 6, 2);
+    load_s(0, x_s);
   }
   __syncthreads();                       // the window's products are complete, its slots free, all nodes looked at
   tc_fence_after();
 
   // ---- linear branch -----------------------------------------------------------------------------------------------
-  // Slots: 0, 1 the remainders of phi(Q); 2, 3 half of S (64 features), leading parts and remainders; 4 phi(K_far), then V_far.
-  const uint32_t sQ = smem_u32(smem), sR = sQ + DA_OFF_RING;
   unsigned char* slots = smem + DA_OFF_RING;
   float* stat = reinterpret_cast<float*>(smem + DA_OFF_STAT);
-  const int k0 = 8 * rank / CS, k1 = 8 * (rank + 1) / CS;    // this CTA's steps of 16 features
-  const float* S = d.state + (size_t)it.z * TILE * TILE;
-  const int corner = max(0, min(dmax, d.w) - age.first);     // far slots: ranks first .. first + corner - 1
   const int n_far = rank == 0 ? corner + bars->n_far_node : 0;
   const bool row_warp = warp < 4 && 32 * warp < it.rows;
-  float inv_phi = 1.f;                                       // of the row's feature map
-
-  // 16 float4 of S per thread (128 threads), then their two halves to slots 2, 3
-  auto load_s = [&](int hh, float4 (&x)[16]) {
-    const int c = tid - 128;
+  auto steps_of = [&](int chunk) { return (min(FAR, n_far - chunk) + 15) >> 4; };
+  // values of the far keys, zero behind the last and for nodes that are not finite: to registers (128 threads, a warp per key),
+  // and over their keys
+  auto load_v = [&](int chunk, uint2 (&u)[FAR / 4]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int f = 64 * hh + (c >> 5) + 4 * i;
-      x[i] = f >= 16 * k0 && f < 16 * k1 ? *reinterpret_cast<const float4*>(S + (size_t)f * TILE + (c & 31) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j = 0; j < FAR / 4; ++j) {
+      const int i = chunk + warp - 4 + 4 * j;
+      u[j] = make_uint2(0u, 0u);
+      if (i < n_far) {
+        u[j] = reinterpret_cast<const uint2*>(far_source(i, true))[lane];
+        if (i >= corner && (not_finite(u[j].x) || not_finite(u[j].y))) u[j] = make_uint2(0u, 0u);
+      }
     }
   };
-  auto store_s = [&](const float4 (&x)[16]) {
-    const int c = tid - 128;
+  auto store_v = [&](const uint2 (&u)[FAR / 4]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      uint2 hi, lo;
-      split2(x[i].x, x[i].y, &hi.x, &lo.x);
-      split2(x[i].z, x[i].w, &hi.y, &lo.y);
-      const uint32_t at = at_half((c >> 5) + 4 * i, (c & 31) >> 1) + (c & 1) * 8;
-      *reinterpret_cast<uint2*>(slots + 2 * HT_BYTES + at) = hi;
-      *reinterpret_cast<uint2*>(slots + 3 * HT_BYTES + at) = lo;
-    }
+    for (int j = 0; j < FAR / 4; ++j) *reinterpret_cast<uint2*>(spare(2) + at_half(warp - 4 + 4 * j, lane >> 1) + (lane & 1) * 8) = u[j];
     fence_proxy_async_smem();
   };
-  // products of the features 64 hh .. 64 hh + 63 with this CTA's part of S (MMA warp)
-  auto mma_state = [&](int hh, bool acc) {
-    constexpr uint32_t idesc = instr_desc(128, 128, 0, 1);
-#pragma unroll
-    for (int term = 0; term < 3; ++term) {                   // phi hi S hi, phi hi S lo, phi lo S hi
-      const uint64_t a0 = kmajor_base(term == 2 ? sR : sQ), b0 = mnmajor_base_h(sR + (term == 1 ? 3 : 2) * HT_BYTES);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (4 * hh + k >= k0 && 4 * hh + k < k1) {
-          mma_bf16(tS, a0 + kstep_k(4 * hh + k, HALF_BYTES), b0 + kstep_mn(k), idesc, acc ? 1u : 0u);
-          acc = true;
-        }
+  // the scores of the far keys become weights: those of corner keys of rank below e and of nodes on the path more than w levels up
+  auto far_weights = [&](int chunk) {
+    uint32_t keep = (uint32_t)below(min(corner, max(e, 0) - age.first) - chunk);
+    for (int i = max(corner - chunk, 0); i < FAR && chunk + i < n_far; ++i) {
+      const int j = bars->far_node[chunk + i - corner];
+      if ((j < 64 ? far0 : far1) >> (j & 63) & 1u) keep |= 1u << i;
     }
-    return acc;
+    float z[32];
+    tmem_ld32(tO + 64 + lanes, z);
+    tmem_wait_ld();
+    uint32_t hi[16], lo[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) split2(keep >> (2 * i) & 1u ? z[2 * i] : 0.f, keep >> (2 * i + 1) & 1u ? z[2 * i + 1] : 0.f, &hi[i], &lo[i]);
+    tmem_st16(tO + 64 + lanes, hi);
+    tmem_st16(tO + 96 + lanes, lo);
+    tmem_wait_st();
+  };
+  auto mma_far_scores = [&](int chunk) {                      // phi(Q) phi(K_far)^T: hi hi, lo hi, hi lo
+    const uint32_t idesc = instr_desc(128, 16 * steps_of(chunk), 0, 0);
+#pragma unroll
+    for (int term = 0; term < 3; ++term) {
+      const uint64_t a0 = kmajor_base(term == 1 ? smem_u32(spare(0)) : sQ), a1 = kmajor_base(term == 1 ? smem_u32(spare(1)) : sQ + HALF_BYTES);
+      const uint64_t b0 = kmajor_base_h(smem_u32(spare(2)) + (term == 2 ? FAR * 128 : 0));
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        mma_bf16(tO + 64, (k < 4 ? a0 : a1) + kstep_k(k & 3, HALF_BYTES), b0 + kstep_k(k, HT_HALF), idesc, (term > 0 || k > 0) ? 1u : 0u);
+    }
   };
 
+
+  uint2 v_far[FAR / 4];
   if (row_warp) {
     // the window output leaves the accumulator
     const uint64_t bad0 = (uint64_t)bars->bad[1] << 32 | bars->bad[0], bad1 = (uint64_t)bars->bad[3] << 32 | bars->bad[2];
@@ -555,160 +699,59 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       }
       tmem_wait_st();
     }
-    // phi(Q): leading parts over Q, remainders to slots 0, 1
-    float mq = 0.f, sq = 0.f;
-    if (d.phi == RATTN_PHI_SOFTMAX) {
-      mq = -INFINITY;
-#pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        const uint4 u = *reinterpret_cast<const uint4*>(smem + at_tile(tid, c));
-        const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mq = fmaxf(mq, fmaxf(__uint_as_float(w4[i] << 16), __uint_as_float(w4[i] & 0xffff0000u)));
-      }
-      mq *= LOG2E;
-    }
-#pragma unroll 4
-    for (int c = 0; c < 16; ++c) {
-      const uint4 u = *reinterpret_cast<const uint4*>(smem + at_tile(tid, c));
-      const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
-      uint32_t hi[4], lo[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float p = __uint_as_float(w4[i] << 16), q = __uint_as_float(w4[i] & 0xffff0000u);
-        if (d.phi == RATTN_PHI_SOFTMAX) {
-          p = ex2(p * LOG2E - mq);
-          q = ex2(q * LOG2E - mq);
-          sq += p + q;
-        } else if (d.phi == RATTN_PHI_RELU) {
-          p = fmaxf(p, 0.f);
-          q = fmaxf(q, 0.f);
-        }
-        split2(p, q, &hi[i], &lo[i]);
-      }
-      *reinterpret_cast<uint4*>(smem + at_tile(tid, c)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      *reinterpret_cast<uint4*>(slots + at_tile(tid, c)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    }
-    if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
-    fence_proxy_async_smem();
   }
 
-  // phi(k) of far keys chunk .. chunk + 31 to slot 4, leading parts to its rows 0 - 31 and remainders to 32 - 63 (a row whose
-  // linear branch is a handful of these shows their rounding: 2^-9 of a weight is as much as the output's own): a warp per
-  // key, lane with 4 features
-  auto far_source = [&](int i, bool is_v) -> const __nv_bfloat16* {
-    if (i < corner) return static_cast<const __nv_bfloat16*>(is_v ? d.v_ring : d.k_ring) + ((size_t)it.z * d.w + age.slot(age.first + i)) * TILE;
-    return static_cast<const __nv_bfloat16*>(is_v ? d.v : d.k) + node_at(d, it.b, it.hk, d.H_kv, bars->far_node[i - corner]);
-  };
-  auto build_k = [&](int chunk) {
-#pragma unroll 4
-    for (int i = warp - 4; i < FAR && chunk + i < n_far; i += 4) {
-      const uint2 u = reinterpret_cast<const uint2*>(far_source(chunk + i, false))[lane];
-      float x[4] = {__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
-      if (d.phi == RATTN_PHI_SOFTMAX) {
-        const float m = wmax(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-        float s = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s += x[j] = ex2((x[j] - m) * LOG2E);
-        const float inv = 1.f / wsum(s);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] *= inv;
-      } else if (d.phi == RATTN_PHI_RELU) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = fmaxf(x[j], 0.f);
+  else if (warp >= 4) {
+    // phi(Q) S meanwhile, half of the features after the other
+    if (warp == 4) load_s(0, x_s);
+    bool acc = false;
+#pragma unroll 1
+    for (int hh = 0; hh < 2; ++hh) {
+      if (hh == 1) {
+        mbar_wait(&bars->done, 0u, &bars->abort);
+        __syncwarp();
       }
-      uint2 hi, lo;
-      split2(x[0], x[1], &hi.x, &lo.x);
-      split2(x[2], x[3], &hi.y, &lo.y);
-      unsigned char* to = slots + 4 * HT_BYTES + at_half(i, lane >> 1) + (lane & 1) * 8;
-      *reinterpret_cast<uint2*>(to) = hi;
-      *reinterpret_cast<uint2*>(to + FAR * 128) = lo;
-    }
-    fence_proxy_async_smem();
-  };
-  auto steps_of = [&](int chunk) { return (min(FAR, n_far - chunk) + 15) >> 4; };
-  // values of the far keys to slot 4, zero behind the last and for nodes that are not finite
-  auto build_v = [&](int chunk) {
-#pragma unroll 4
-    for (int i = warp - 4; i < 16 * steps_of(chunk); i += 4) {
-      uint2 u = make_uint2(0u, 0u);
-      if (chunk + i < n_far) {
-        u = reinterpret_cast<const uint2*>(far_source(chunk + i, true))[lane];
-        if (chunk + i >= corner && (not_finite(u.x) || not_finite(u.y))) u = make_uint2(0u, 0u);
+      store_s(x_s);
+      if (hh == 0) load_s(1, x_s);
+      named_sync(2, 128);
+      if (warp == 4) {
+        tc_fence_after();
+        acc = mma_state(hh, acc);
+        if (hh == 0) mma_commit(&bars->done);
       }
-      *reinterpret_cast<uint2*>(slots + 4 * HT_BYTES + at_half(i, lane >> 1) + (lane & 1) * 8) = u;
     }
-    fence_proxy_async_smem();
-  };
-  // the scores of the far keys become weights: those of corner keys of rank below e and of nodes on the path more than w levels up
-  auto far_weights = [&](int chunk) {
-    uint32_t keep = (uint32_t)below(min(corner, max(e, 0) - age.first) - chunk);
-    for (int i = max(corner - chunk, 0); i < FAR && chunk + i < n_far; ++i) {
-      const int j = bars->far_node[chunk + i - corner];
-      if ((j < 64 ? far0 : far1) >> (j & 63) & 1u) keep |= 1u << i;
-    }
-    float z[32];
-    tmem_ld32(tO + 64 + lanes, z);
-    tmem_wait_ld();
-    uint32_t hi[16], lo[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) split2(keep >> (2 * i) & 1u ? z[2 * i] : 0.f, keep >> (2 * i + 1) & 1u ? z[2 * i + 1] : 0.f, &hi[i], &lo[i]);
-    tmem_st16(tO + 64 + lanes, hi);
-    tmem_st16(tO + 96 + lanes, lo);
-    tmem_wait_st();
-  };
-  auto mma_far_scores = [&](int chunk) {                      // phi(Q) phi(K_far)^T: hi hi, lo hi, hi lo
-    const uint32_t idesc = instr_desc(128, 16 * steps_of(chunk), 0, 0);
-#pragma unroll
-    for (int term = 0; term < 3; ++term) {
-      const uint64_t a0 = kmajor_base(term == 1 ? sR : sQ), b0 = kmajor_base_h(sR + 4 * HT_BYTES + (term == 2 ? FAR * 128 : 0));
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        mma_bf16(tO + 64, a0 + kstep_k(k, HALF_BYTES), b0 + kstep_k(k, HT_HALF), idesc, (term > 0 || k > 0) ? 1u : 0u);
-    }
-  };
-
-  // A: phi(Q), the first half of S and the first far keys are in place
-  float4 x[16];
-  if (warp >= 4) {
-    load_s(0, x);
-    store_s(x);
-    load_s(1, x);
-    build_k(0);
+    load_v(0, v_far);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  bool acc = false;
+  uint32_t done_phase = 1;
   if (warp == 4) {
-    acc = mma_state(0, false);
     if (n_far > 0) mma_far_scores(0);
     mma_commit(&bars->done);
   }
-  mbar_wait(&bars->done, 0u, &bars->abort);
-  __syncwarp();
-  tc_fence_after();
-  // B: the second half of S over the first, the values of the far keys over their keys, the weights over their scores
-  if (warp >= 4) {
-    store_s(x);
-    if (n_far > 0) build_v(0);
-  } else if (row_warp && n_far > 0) {
-    far_weights(0);
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (warp == 4) {
-    mma_state(1, acc);
-    if (n_far > 0) mma_weights(tS, tO + 64, sR + 4 * HT_BYTES, true, steps_of(0));
-    mma_commit(&bars->done);
-  }
-  uint32_t done_phase = 1;
   mbar_wait(&bars->done, 1u, &bars->abort);
   __syncwarp();
   tc_fence_after();
+  if (n_far > 0) {                                           // (the same for all threads)
+    if (warp >= 4) store_v(v_far);
+    else if (row_warp) far_weights(0);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 4) {
+      mma_weights(tS, tO + 64, smem_u32(spare(2)), true, steps_of(0));
+      mma_commit(&bars->done);
+    }
+    mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
+    __syncwarp();
+    tc_fence_after();
+  }
   for (int chunk = FAR; chunk < n_far; chunk += FAR) {       // trees deep enough for more of them (the same for all threads)
-    if (warp >= 4) build_k(chunk);
+    if (warp >= 4) {
+      build_k(chunk, n_far, 4, 4);
+      load_v(chunk, v_far);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -719,13 +762,13 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
     __syncwarp();
     tc_fence_after();
-    if (warp >= 4) build_v(chunk);
+    if (warp >= 4) store_v(v_far);
     else if (row_warp) far_weights(chunk);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == 4) {
-      mma_weights(tS, tO + 64, sR + 4 * HT_BYTES, true, steps_of(chunk));
+      mma_weights(tS, tO + 64, smem_u32(spare(2)), true, steps_of(chunk));
       mma_commit(&bars->done);
     }
     mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
@@ -822,23 +865,32 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     // Head by head, so that its gains are read once; a warp takes every eighth of a head's rows, which are G apart.
     const int c0 = 4 * lane, n0 = small_div(it.row0, a.inv_group), g0 = it.row0 - n0 * G;
     const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+    auto gain_of = [&](const float* gamma, int i) {
+      const int g = g0 + i, h = it.hk * G + (g >= G ? g - G : g);
+      return gamma && i < G ? *reinterpret_cast<const float4*>(gamma + (size_t)h * TILE + c0) : one;
+    };
+    float4 gs = gain_of(d.gamma_swa, 0), gr = gain_of(d.gamma_rla, 0);
+    const size_t step = (d.layout == RATTN_LAYOUT_BHTD ? (size_t)TILE : (size_t)d.H_q * TILE) * (DA_THREADS / 32);
+#pragma unroll 1
     for (int i = 0; i < G && i < it.rows; ++i) {             // rows i, i + G, ..: head g of nodes n, n + 1, ..
-      const int wrap = g0 + i >= G, g = g0 + i - (wrap ? G : 0), h = it.hk * G + g;
-      const float4 gs = d.gamma_swa ? *reinterpret_cast<const float4*>(d.gamma_swa + (size_t)h * TILE + c0) : one;
-      const float4 gr = d.gamma_rla ? *reinterpret_cast<const float4*>(d.gamma_rla + (size_t)h * TILE + c0) : one;
-      // (the first row of warp `warp` among them; heads in turn start with another warp, so that short ones are shared out)
-      const int k0 = (warp - i) & 7;
+      const float4 gs_next = gain_of(d.gamma_swa, i + 1), gr_next = gain_of(d.gamma_rla, i + 1);
+      const int wrap = g0 + i >= G, h = it.hk * G + g0 + i - (wrap ? G : 0);
+      // (heads in turn start with another warp, so that few rows are shared out)
+      const int k0_ = (warp - i) & 7;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n0 + wrap + k0_) + c0;
 #pragma unroll 2
-      for (int k = k0; i + G * k < it.rows; k += DA_THREADS / 32) {
-        const int r = i + G * k, n = n0 + wrap + k;
-        if (bars->depth[n] < 0) continue;
+      for (int k = k0_; i + G * k < it.rows; k += DA_THREADS / 32, out += step) {
+        const int r = i + G * k;
+        if (bars->depth[n0 + wrap + k] < 0) continue;
         const short4 u = *reinterpret_cast<const short4*>(smem + at_row(r, lane >> 1) + (lane & 1) * 8);
         const float4 y = *reinterpret_cast<const float4*>(slots + at_ox(r, lane));
         const float unit = bars->odd[r] ? __uint_as_float(0x7fc00000u) : 1.f / PARK;
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
+        *reinterpret_cast<uint2*>(out) =
             make_uint2(pack_bf16(gs.x * ((float)u.x * unit) + gr.x * y.x, gs.y * ((float)u.y * unit) + gr.y * y.y),
                        pack_bf16(gs.z * ((float)u.z * unit) + gr.z * y.z, gs.w * ((float)u.w * unit) + gr.w * y.w));
       }
+      gs = gs_next;
+      gr = gr_next;
     }
    }
   }
