@@ -9,9 +9,11 @@
 //
 // A batch entry has a cluster of CTAs; each takes a run of the vocabulary, each of its warps a run of that.  All threads of the
 // cluster walk the tree alike (from shared memory; the sums are added in an order fixed by the sizes), so
-// nothing but the partial sums passes between them, through distributed shared memory.  r is never stored: it is formed
-// again from p, q and the list of Z.  Sums, r and comparisons are fp64: the drawn token is an index, and in fp32 the
-// running sum over 10^5 tokens of 10^-5 would be off by as much as their probabilities.
+// nothing but the partial sums passes between them, through distributed shared memory.  r is never stored: q being at least 0,
+// max(max(p - a q, 0) - b q, 0) = max(p - (a + b) q, 0), so r after any number of rejections is formed from p, q and the sum
+// of their Z.  A thread asks for 64 bytes or more of either row before it uses the first of them.  Sums, r and comparisons are
+// fp64: the drawn token is an index, and in fp32 the running sum over 10^5 tokens of 10^-5 would be off by as much as
+// their probabilities.
 #include "draft_internal.h"
 
 namespace rattn {
@@ -28,10 +30,28 @@ struct VerifyArgs {
   int B, N, V;
 };
 
-template <typename T> __device__ __forceinline__ float prob(T x) {      // negative and NaN count as 0
-  const float f = (float)x;
-  return f > 0.f ? f : 0.f;
-}
+__device__ __forceinline__ float prob(float f) { return f > 0.f ? f : 0.f; }      // negative and NaN count as 0
+
+// VEC consecutive probabilities; VEC = 1 where rows do not start on 16-byte boundaries
+template <typename T, int VEC> struct Probs;
+template <typename T> struct Probs<T, 1> {
+  T raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *p; }
+  __device__ __forceinline__ float at(int) const { return prob((float)raw); }
+};
+template <> struct Probs<float, 4> {
+  float4 raw;
+  __device__ __forceinline__ void load(const float* p) { raw = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ float at(int i) const { return prob(i == 0 ? raw.x : i == 1 ? raw.y : i == 2 ? raw.z : raw.w); }
+};
+template <> struct Probs<__nv_bfloat16, 8> {
+  uint4 raw;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { raw = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ float at(int i) const {
+    const uint32_t w = i < 2 ? raw.x : i < 4 ? raw.y : i < 6 ? raw.z : raw.w;
+    return prob(__uint_as_float((i & 1) ? w & 0xffff0000u : w << 16));
+  }
+};
 
 __device__ __forceinline__ double wsum(double x) {
 #pragma unroll
@@ -52,24 +72,17 @@ __device__ __forceinline__ double ld_cluster(const double* p, int rank) {
 
 // What the rejections under the current node have left of its row.
 struct Left {
-  int n;                         // rejections that count
-  double Z[kMaxNodes];           // with a drafter's row: Z ahead of each of them
-  int x[kMaxNodes];              // without: the token that each of them took out
+  int n;                         // without a drafter's row: tokens taken out
+  int x[kMaxNodes];
 };
-
-template <typename T, bool DRAFT>
-__device__ __forceinline__ double left_of(double p, double q, int x, const Left& l) {
-  if (DRAFT) {
-    for (int i = 0; i < l.n; ++i) p = fmax(p - l.Z[i] * q, 0.0);
-  } else {
-    for (int i = 0; i < l.n; ++i)
-      if (l.x[i] == x) p = 0.0;
-  }
-  return p;
+__device__ __forceinline__ bool taken_out(const Left& l, int x) {
+  for (int i = 0; i < l.n; ++i)
+    if (l.x[i] == x) return true;
+  return false;
 }
 
-template <typename T, bool DRAFT>
-__global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_constant__ VerifyArgs a) {
+template <typename T, bool DRAFT, int VEC>
+__global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __grid_constant__ VerifyArgs a) {
   __shared__ int par[kMaxNodes], tok[kMaxNodes], path[kMaxNodes];
   __shared__ float u_s[kMaxNodes];
   __shared__ double pt[kMaxNodes], qt[kMaxNodes];
@@ -88,8 +101,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
     tok[tid] = x;
     u_s[tid] = a.u[(size_t)b * N + tid];
     const bool real = up >= 0 && up < tid && x >= 0 && x < V;
-    pt[tid] = real ? (double)prob(p_rows[(size_t)up * V + x]) : 0.0;
-    qt[tid] = DRAFT ? (real ? (double)prob(q_rows[(size_t)up * V + x]) : 0.0) : 1.0;
+    pt[tid] = real ? (double)prob((float)p_rows[(size_t)up * V + x]) : 0.0;
+    qt[tid] = DRAFT ? (real ? (double)prob((float)q_rows[(size_t)up * V + x]) : 0.0) : 1.0;
   }
   if (tid == 0) left.n = 0;
   __syncthreads();
@@ -105,35 +118,70 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
     }
     return;
   }
-  // runs of the vocabulary: this CTA's, this warp's
-  const int per_cta = (V + DV_CLUSTER - 1) / DV_CLUSTER, per_warp = (per_cta + DV_WARPS - 1) / DV_WARPS;
+  // Runs of the vocabulary: this CTA's, this warp's, in steps of 32 lanes x VEC tokens.
+  constexpr int STEP = 32 * VEC, AHEAD = VEC == 1 ? 8 : 4;
+  const int per_warp = (V + DV_CLUSTER * DV_WARPS * STEP - 1) / (DV_CLUSTER * DV_WARPS * STEP) * STEP, per_cta = per_warp * DV_WARPS;
   const int cta0 = min(rank * per_cta, V), cta1 = min(cta0 + per_cta, V);
   const int w0 = min(cta0 + warp * per_warp, cta1), w1 = min(w0 + per_warp, cta1);
   int turn = 0;
-  // Sum of r over the vocabulary, with a rejection at Z that is not in the list yet (draft rows; pending).  Leaves the
-  // warps' sums in warp_sum and the CTAs' in cta_sum[turn - 1].
-  auto total = [&](int c, bool pending, double Z) -> double {
+  double gone = 0.0;                                        // the sum of Z over the rejections that count
+  // r of VEC tokens from x on, after rejections of `taken` in all; tokens behind the row's end have none
+  auto left_of = [&](const Probs<T, VEC>& p, const Probs<T, VEC>& q, int x, int end, double taken, bool check, double (&r)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      r[i] = (double)p.at(i);
+      if (DRAFT) r[i] = fmax(r[i] - taken * (double)q.at(i), 0.0);
+      else if (check && taken_out(left, x + i)) r[i] = 0.0;
+      if (x + i >= end) r[i] = 0.0;
+    }
+  };
+  // whether one of the tokens x .. x + n - 1 has been taken out
+  auto any_out = [&](int x, int n) {
+    bool any = false;
+    if (!DRAFT)
+      for (int i = 0; i < left.n; ++i) any |= (unsigned)(left.x[i] - x) < (unsigned)n;
+    return any;
+  };
+  // Sum of r over the vocabulary.  Leaves the warps' sums in warp_sum and the CTAs' in cta_sum[turn - 1].  (Rows start on
+  // 16-byte boundaries where VEC > 1, and then their lengths are multiples of VEC.)
+  auto total = [&](int c, double taken) -> double {
     const T* p = p_rows + (size_t)c * V;
     const T* q = q_rows + (size_t)c * V;
     double s = 0.0;
-#pragma unroll 4
-    for (int x = w0 + lane; x < w1; x += 32) {
-      const double qx = DRAFT ? (double)prob(q[x]) : 0.0;
-      double r = left_of<T, DRAFT>((double)prob(p[x]), qx, x, left);
-      if (DRAFT && pending) r = fmax(r - Z * qx, 0.0);
-      s += r;
+#pragma unroll 1
+    for (int base = w0; base < w1; base += AHEAD * STEP) {
+      Probs<T, VEC> pv[AHEAD], qv[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int x = min(base + j * STEP + lane * VEC, V - VEC);       // (what lies behind the run is not counted)
+        pv[j].load(p + x);
+        if (DRAFT) qv[j].load(q + x);
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        double r[VEC];
+        const int x = base + j * STEP + lane * VEC;
+        left_of(pv[j], qv[j], x, w1, taken, any_out(base + j * STEP, STEP), r);
+        if (VEC == 1) s += r[0];
+        else
+#pragma unroll
+          for (int i = 0; i < VEC; i += 4) s += (r[i] + r[i + 1 < VEC ? i + 1 : i]) + (r[i + 2 < VEC ? i + 2 : i] + r[i + 3 < VEC ? i + 3 : i]);
+      }
     }
     s = wsum(s);
     if (lane == 0) warp_sum[warp] = s;
     __syncthreads();
-    if (tid == 0) {
-      double t = 0.0;
-      for (int i = 0; i < DV_WARPS; ++i) t += warp_sum[i];
-      cta_sum[turn & 1] = t;
+    if (warp == 0) {
+      double t = lane < DV_WARPS ? warp_sum[lane] : 0.0;
+      t = wsum(t);
+      if (lane == 0) cta_sum[turn & 1] = t;
     }
     cluster_sync();
-    double t = 0.0;
-    for (int r = 0; r < DV_CLUSTER; ++r) t += ld_cluster(&cta_sum[turn & 1], r);
+    double part[DV_CLUSTER], t = 0.0;
+#pragma unroll
+    for (int r = 0; r < DV_CLUSTER; ++r) part[r] = ld_cluster(&cta_sum[turn & 1], r);
+#pragma unroll
+    for (int r = 0; r < DV_CLUSTER; ++r) t += part[r];
     ++turn;
     return t;
   };
@@ -144,12 +192,10 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
   bool pending = false, summed = false;                     // summed: the last pass was over r as it is now
   // a rejection whose sum has not been formed
   auto settle = [&]() {
-    const double s = total(c, true, Z);
+    const double s = total(c, gone + Z);
     const bool counts = s > kTiny * Z;
     if (counts) {
-      __syncthreads();
-      if (tid == 0) left.Z[left.n++] = Z;
-      __syncthreads();
+      gone += Z;
       Z = s;
     }
     pending = false;
@@ -162,10 +208,11 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
     const int x = tok[i];
     if (x < 0 || x >= V) continue;
     if (pending) settle();
-    const double r = left_of<T, DRAFT>(pt[i], qt[i], x, left);
+    const double r = DRAFT ? fmax(pt[i] - gone * qt[i], 0.0) : taken_out(left, x) ? 0.0 : pt[i];
     if ((double)u_s[i] * qt[i] * Z < r) {
       c = i;
       Z = 1.0;
+      gone = 0.0;
       __syncthreads();
       if (tid == 0) {
         left.n = 0;
@@ -184,12 +231,13 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
     }
   }
   if (DRAFT && pending) settle();
-  if (!summed) sum = total(c, false, 0.0);
-  if (!(sum > 0.0) && left.n > 0) {                         // nothing left: the row as it is given
+  if (!summed) sum = total(c, gone);
+  if (!(sum > 0.0) && (gone > 0.0 || left.n > 0)) {         // nothing left: the row as it is given
     __syncthreads();
     if (tid == 0) left.n = 0;
     __syncthreads();
-    sum = total(c, false, 0.0);
+    gone = 0.0;
+    sum = total(c, 0.0);
   }
   // the draw: the CTA, the warp and the token in whose share the target lies
   if (!(sum > 0.0)) {
@@ -222,21 +270,43 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
       const int x0 = min(cta0 + mine * per_warp, cta1), x1 = min(x0 + per_warp, cta1);
       int found = -1, last_x = -1;
       run = ahead;
-      for (int base = x0; base < x1 && found < 0; base += 32) {
-        const int x = base + lane;
-        double r = 0.0;
-        if (x < x1) r = left_of<T, DRAFT>((double)prob(p[x]), DRAFT ? (double)prob(q[x]) : 0.0, x, left);
-        double s = r;
+      for (int base = x0; base < x1 && found < 0; base += STEP) {
+        const int x = base + lane * VEC, at = min(x, V - VEC);
+        Probs<T, VEC> pv, qv;
+        pv.load(p + at);
+        if (DRAFT) qv.load(q + at);
+        double r[VEC], s = 0.0;
+        left_of(pv, qv, x, x1, gone, any_out(base, STEP), r);
+        bool mine_any = false;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          s += r[i];
+          mine_any |= r[i] > 0.0;
+        }
+        double upto = s;                                     // of the lanes up to this one
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const double t = __shfl_up_sync(0xffffffffu, s, o);
-          if (lane >= o) s += t;
+          const double t = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += t;
         }
-        const uint32_t some = __ballot_sync(0xffffffffu, r > 0.0);
-        const uint32_t hit = __ballot_sync(0xffffffffu, r > 0.0 && run + s > target);
-        if (some) last_x = base + 31 - __clz(some);
-        if (!beyond && hit) found = base + __ffs(hit) - 1;
-        run += __shfl_sync(0xffffffffu, s, 31);
+        int last_i = -1, hit_i = -1;
+        double t = run + (upto - s);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          t += r[i];
+          if (r[i] > 0.0) last_i = i;
+          if (hit_i < 0 && r[i] > 0.0 && t > target) hit_i = i;
+        }
+        const uint32_t some = __ballot_sync(0xffffffffu, mine_any), hit = __ballot_sync(0xffffffffu, hit_i >= 0);
+        if (some) {
+          const int from = 31 - __clz(some);
+          last_x = base + from * VEC + __shfl_sync(0xffffffffu, last_i, from);
+        }
+        if (!beyond && hit) {
+          const int from = __ffs(hit) - 1;
+          found = base + from * VEC + __shfl_sync(0xffffffffu, hit_i, from);
+        }
+        run += __shfl_sync(0xffffffffu, upto, 31);
       }
       if (lane == 0) a.token[b] = found >= 0 ? found : last_x;
     }
@@ -248,19 +318,20 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const __grid_c
   cluster_sync();                                           // nobody leaves while its sums are being read
 }
 
-template <typename T, bool DRAFT>
+template <typename T, bool DRAFT, int VEC>
 cudaError_t launch_verify(const VerifyArgs& a, cudaStream_t s) {
   KernelTimer kt("draft_verify", s);
-  const cudaError_t e = launch_pdl_cluster(draft_verify_kernel<T, DRAFT>, dim3((unsigned)(a.B * DV_CLUSTER)), dim3(DV_THREADS), 0, s,
+  const cudaError_t e = launch_pdl_cluster(draft_verify_kernel<T, DRAFT, VEC>, dim3((unsigned)(a.B * DV_CLUSTER)), dim3(DV_THREADS), 0, s,
                                            true, DV_CLUSTER, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   return cudaGetLastError();
 }
 
-template <typename T>
+template <typename T, int VEC>
 cudaError_t launch_verify_as(const VerifyArgs& a, cudaStream_t s) {
-  return a.q ? launch_verify<T, true>(a, s) : launch_verify<T, false>(a, s);
+  if (a.V % VEC) return a.q ? launch_verify<T, true, 1>(a, s) : launch_verify<T, false, 1>(a, s);
+  return a.q ? launch_verify<T, true, VEC>(a, s) : launch_verify<T, false, VEC>(a, s);
 }
 
 bool misaligned(const void* p, unsigned by) { return ((uintptr_t)p & (by - 1)) != 0; }
@@ -287,7 +358,7 @@ extern "C" int rattn_draft_verify(const rattn_verify_params* p, void* stream) {
   a.path = p->path; a.n_accepted = p->n_accepted; a.token = p->token;
   a.B = p->B; a.N = p->N; a.V = p->V;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->dtype == RATTN_BF16 ? launch_verify_as<__nv_bfloat16>(a, s) : launch_verify_as<float>(a, s);
+  const cudaError_t e = p->dtype == RATTN_BF16 ? launch_verify_as<__nv_bfloat16, 8>(a, s) : launch_verify_as<float, 4>(a, s);
   if (e == cudaSuccess) return RATTN_OK;
   set_last_cuda_error((int)e);
   return RATTN_ERR_CUDA;
