@@ -14,6 +14,8 @@
 // of their Z.  A thread asks for 64 bytes or more of either row before it uses the first of them.  Sums, r and comparisons are
 // fp64: the drawn token is an index, and in fp32 the running sum over 10^5 tokens of 10^-5 would be off by as much as
 // their probabilities.
+
+
 #include "draft_internal.h"
 
 namespace rattn {
@@ -32,21 +34,29 @@ struct VerifyArgs {
 
 __device__ __forceinline__ float prob(float f) { return f > 0.f ? f : 0.f; }      // negative and NaN count as 0
 
-// VEC consecutive probabilities; VEC = 1 where rows do not start on 16-byte boundaries
-template <typename T, int VEC> struct Probs;
-template <typename T> struct Probs<T, 1> {
-  T raw;
-  __device__ __forceinline__ void load(const T* p) { raw = *p; }
-  __device__ __forceinline__ float at(int) const { return prob((float)raw); }
-};
-template <> struct Probs<float, 4> {
+// 16 bytes of a row.  A row of a vocabulary of any size may start anywhere, so a row is walked from the 16-byte boundary at or
+// before its start (what lies there is the row ahead of it) and its last few probabilities are read one by one.
+template <typename T> struct Probs;
+template <> struct Probs<float> {
+  static constexpr int N = 4;
   float4 raw;
   __device__ __forceinline__ void load(const float* p) { raw = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void load_some(const float* p, int n) {
+    raw = make_float4(n > 0 ? p[0] : 0.f, n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, 0.f);
+  }
   __device__ __forceinline__ float at(int i) const { return prob(i == 0 ? raw.x : i == 1 ? raw.y : i == 2 ? raw.z : raw.w); }
 };
-template <> struct Probs<__nv_bfloat16, 8> {
+template <> struct Probs<__nv_bfloat16> {
+  static constexpr int N = 8;
   uint4 raw;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { raw = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load_some(const __nv_bfloat16* p, int n) {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < n) w[i >> 1] |= (uint32_t)__bfloat16_as_ushort(p[i]) << (16 * (i & 1));
+    raw = make_uint4(w[0], w[1], w[2], w[3]);
+  }
   __device__ __forceinline__ float at(int i) const {
     const uint32_t w = i < 2 ? raw.x : i < 4 ? raw.y : i < 6 ? raw.z : raw.w;
     return prob(__uint_as_float((i & 1) ? w & 0xffff0000u : w << 16));
@@ -81,7 +91,7 @@ __device__ __forceinline__ bool taken_out(const Left& l, int x) {
   return false;
 }
 
-template <typename T, bool DRAFT, int VEC>
+template <typename T, bool DRAFT>
 __global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __grid_constant__ VerifyArgs a) {
   __shared__ int par[kMaxNodes], tok[kMaxNodes], path[kMaxNodes];
   __shared__ float u_s[kMaxNodes];
@@ -119,20 +129,32 @@ __global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __gri
     return;
   }
   // Runs of the vocabulary: this CTA's, this warp's, in steps of 32 lanes x VEC tokens.
-  constexpr int STEP = 32 * VEC, AHEAD = VEC == 1 ? 8 : 4;
-  const int per_warp = (V + DV_CLUSTER * DV_WARPS * STEP - 1) / (DV_CLUSTER * DV_WARPS * STEP) * STEP, per_cta = per_warp * DV_WARPS;
-  const int cta0 = min(rank * per_cta, V), cta1 = min(cta0 + per_cta, V);
-  const int w0 = min(cta0 + warp * per_warp, cta1), w1 = min(w0 + per_warp, cta1);
+  // (Places in a row: token x of node c's row is at place x + shift, shift = c V modulo VEC.)
+  constexpr int VEC = Probs<T>::N, STEP = 32 * VEC, AHEAD = 4;
+  const int per_warp = (V + VEC - 1 + DV_CLUSTER * DV_WARPS * STEP - 1) / (DV_CLUSTER * DV_WARPS * STEP) * STEP, per_cta = per_warp * DV_WARPS;
+  const int w0 = rank * per_cta + warp * per_warp;
   int turn = 0;
   double gone = 0.0;                                        // the sum of Z over the rejections that count
-  // r of VEC tokens from x on, after rejections of `taken` in all; tokens behind the row's end have none
-  auto left_of = [&](const Probs<T, VEC>& p, const Probs<T, VEC>& q, int x, int end, double taken, bool check, double (&r)[VEC]) {
+  auto shift_of = [&](int c) { return (int)(((size_t)b * N + c) * V % VEC); };
+  // the VEC probabilities at place k of a row; row: its place 0
+  auto fetch = [&](Probs<T>* v, const T* row, int k, int end) {
+    if (k + VEC <= end) v->load(row + k);
+    else v->load_some(row + k, end - k);
+  };
+  // r of VEC tokens from x on, after rejections of `taken` in all.  edge: some of them may lie in front of the row or behind it,
+  // where there is none.
+  auto left_of = [&](const Probs<T>& p, const Probs<T>& q, int x, double taken, bool check, double (&r)[VEC], bool edge) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       r[i] = (double)p.at(i);
-      if (DRAFT) r[i] = fmax(r[i] - taken * (double)q.at(i), 0.0);
-      else if (check && taken_out(left, x + i)) r[i] = 0.0;
-      if (x + i >= end) r[i] = 0.0;
+      if (DRAFT) {
+        r[i] = r[i] - taken * (double)q.at(i);
+        const int hi = __double2hiint(r[i]), keep = ~(hi >> 31);       // max(r, 0)
+        r[i] = __hiloint2double(hi & keep, __double2loint(r[i]) & keep);
+      } else if (check && taken_out(left, x + i)) {
+        r[i] = 0.0;
+      }
+      if (edge && (unsigned)(x + i) >= (unsigned)V) r[i] = 0.0;
     }
   };
   // whether one of the tokens x .. x + n - 1 has been taken out
@@ -142,32 +164,42 @@ __global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __gri
       for (int i = 0; i < left.n; ++i) any |= (unsigned)(left.x[i] - x) < (unsigned)n;
     return any;
   };
-  // Sum of r over the vocabulary.  Leaves the warps' sums in warp_sum and the CTAs' in cta_sum[turn - 1].  (Rows start on
-  // 16-byte boundaries where VEC > 1, and then their lengths are multiples of VEC.)
+  // Sum of r over the vocabulary.  Leaves the warps' sums in warp_sum and the CTAs' in cta_sum[turn - 1].
   auto total = [&](int c, double taken) -> double {
-    const T* p = p_rows + (size_t)c * V;
-    const T* q = q_rows + (size_t)c * V;
+    const int shift = shift_of(c), end = V + shift, w1 = min(w0 + per_warp, end);
+    const T* p = p_rows + (size_t)c * V - shift;
+    const T* q = q_rows + (size_t)c * V - shift;
     double s = 0.0;
-#pragma unroll 1
-    for (int base = w0; base < w1; base += AHEAD * STEP) {
-      Probs<T, VEC> pv[AHEAD], qv[AHEAD];
+    auto add = [&](const Probs<T>& pv, const Probs<T>& qv, int base, bool edge) {
+      double r[VEC];
+      left_of(pv, qv, base + lane * VEC - shift, taken, any_out(base - shift, STEP), r, edge);
 #pragma unroll
-      for (int j = 0; j < AHEAD; ++j) {
-        const int x = min(base + j * STEP + lane * VEC, V - VEC);       // (what lies behind the run is not counted)
-        pv[j].load(p + x);
-        if (DRAFT) qv[j].load(q + x);
-      }
-#pragma unroll
-      for (int j = 0; j < AHEAD; ++j) {
-        double r[VEC];
-        const int x = base + j * STEP + lane * VEC;
-        left_of(pv[j], qv[j], x, w1, taken, any_out(base + j * STEP, STEP), r);
-        if (VEC == 1) s += r[0];
-        else
-#pragma unroll
-          for (int i = 0; i < VEC; i += 4) s += (r[i] + r[i + 1 < VEC ? i + 1 : i]) + (r[i + 2 < VEC ? i + 2 : i] + r[i + 3 < VEC ? i + 3 : i]);
-      }
+      for (int i = 0; i < VEC; i += 4) s += (r[i] + r[i + 1]) + (r[i + 2] + r[i + 3]);
+    };
+    auto some = [&](int base) {                             // a step at an end of the row
+      Probs<T> pv, qv;
+      fetch(&pv, p, base + lane * VEC, end);
+      if (DRAFT) fetch(&qv, q, base + lane * VEC, end);
+      add(pv, qv, base, true);
+    };
+    int base = w0;
+    if (base == 0 && shift > 0 && w1 > 0) {
+      some(0);
+      base = STEP;
     }
+#pragma unroll 1
+    for (; base + AHEAD * STEP <= w1; base += AHEAD * STEP) {          // whole vectors
+      Probs<T> pv[AHEAD], qv[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        pv[j].load(p + base + j * STEP + lane * VEC);
+        if (DRAFT) qv[j].load(q + base + j * STEP + lane * VEC);
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) add(pv[j], qv[j], base + j * STEP, false);
+    }
+#pragma unroll 1
+    for (; base < w1; base += STEP) some(base);
     s = wsum(s);
     if (lane == 0) warp_sum[warp] = s;
     __syncthreads();
@@ -265,18 +297,19 @@ __global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __gri
         run += s;
       }
       if (mine < 0) { mine = last; beyond = true; }
-      const T* p = p_rows + (size_t)c * V;
-      const T* q = q_rows + (size_t)c * V;
-      const int x0 = min(cta0 + mine * per_warp, cta1), x1 = min(x0 + per_warp, cta1);
+      const int shift = shift_of(c), end = V + shift;
+      const T* p = p_rows + (size_t)c * V - shift;
+      const T* q = q_rows + (size_t)c * V - shift;
+      const int k0 = rank * per_cta + mine * per_warp, k1 = min(k0 + per_warp, end);
       int found = -1, last_x = -1;
       run = ahead;
-      for (int base = x0; base < x1 && found < 0; base += STEP) {
-        const int x = base + lane * VEC, at = min(x, V - VEC);
-        Probs<T, VEC> pv, qv;
-        pv.load(p + at);
-        if (DRAFT) qv.load(q + at);
+      for (int base = k0; base < k1 && found < 0; base += STEP) {
+        const int k = base + lane * VEC;
+        Probs<T> pv, qv;
+        fetch(&pv, p, k, end);
+        if (DRAFT) fetch(&qv, q, k, end);
         double r[VEC], s = 0.0;
-        left_of(pv, qv, x, x1, gone, any_out(base, STEP), r);
+        left_of(pv, qv, k - shift, gone, any_out(base - shift, STEP), r, true);
         bool mine_any = false;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -300,11 +333,11 @@ __global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __gri
         const uint32_t some = __ballot_sync(0xffffffffu, mine_any), hit = __ballot_sync(0xffffffffu, hit_i >= 0);
         if (some) {
           const int from = 31 - __clz(some);
-          last_x = base + from * VEC + __shfl_sync(0xffffffffu, last_i, from);
+          last_x = base - shift + from * VEC + __shfl_sync(0xffffffffu, last_i, from);
         }
         if (!beyond && hit) {
           const int from = __ffs(hit) - 1;
-          found = base + from * VEC + __shfl_sync(0xffffffffu, hit_i, from);
+          found = base - shift + from * VEC + __shfl_sync(0xffffffffu, hit_i, from);
         }
         run += __shfl_sync(0xffffffffu, upto, 31);
       }
@@ -318,20 +351,19 @@ __global__ void __launch_bounds__(DV_THREADS, 2) draft_verify_kernel(const __gri
   cluster_sync();                                           // nobody leaves while its sums are being read
 }
 
-template <typename T, bool DRAFT, int VEC>
+template <typename T, bool DRAFT>
 cudaError_t launch_verify(const VerifyArgs& a, cudaStream_t s) {
   KernelTimer kt("draft_verify", s);
-  const cudaError_t e = launch_pdl_cluster(draft_verify_kernel<T, DRAFT, VEC>, dim3((unsigned)(a.B * DV_CLUSTER)), dim3(DV_THREADS), 0, s,
+  const cudaError_t e = launch_pdl_cluster(draft_verify_kernel<T, DRAFT>, dim3((unsigned)(a.B * DV_CLUSTER)), dim3(DV_THREADS), 0, s,
                                            true, DV_CLUSTER, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   return cudaGetLastError();
 }
 
-template <typename T, int VEC>
+template <typename T>
 cudaError_t launch_verify_as(const VerifyArgs& a, cudaStream_t s) {
-  if (a.V % VEC) return a.q ? launch_verify<T, true, 1>(a, s) : launch_verify<T, false, 1>(a, s);
-  return a.q ? launch_verify<T, true, VEC>(a, s) : launch_verify<T, false, VEC>(a, s);
+  return a.q ? launch_verify<T, true>(a, s) : launch_verify<T, false>(a, s);
 }
 
 bool misaligned(const void* p, unsigned by) { return ((uintptr_t)p & (by - 1)) != 0; }
@@ -358,7 +390,7 @@ extern "C" int rattn_draft_verify(const rattn_verify_params* p, void* stream) {
   a.path = p->path; a.n_accepted = p->n_accepted; a.token = p->token;
   a.B = p->B; a.N = p->N; a.V = p->V;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->dtype == RATTN_BF16 ? launch_verify_as<__nv_bfloat16, 8>(a, s) : launch_verify_as<float, 4>(a, s);
+  const cudaError_t e = p->dtype == RATTN_BF16 ? launch_verify_as<__nv_bfloat16>(a, s) : launch_verify_as<float>(a, s);
   if (e == cudaSuccess) return RATTN_OK;
   set_last_cuda_error((int)e);
   return RATTN_ERR_CUDA;
