@@ -3,11 +3,12 @@
 //   S += sum_a phi(k_old(a))^T v_old(a),     ring slot (pos + a) % w = token a,        a = 0 .. n-1,
 //
 // old(a) = token pos + a - w: a ring slot's for a < w, an accepted token's behind that.  One read and one write of the
-// state (64 KB each at d = 128) is nearly all of the traffic, so HBM bounds it, or latency for few heads: a (batch entry, K/V
-// head) is shared by a cluster of CTAs, each with a share of the state's rows in registers, requested before anything else.
+// state (64 KB each at d = 128) is nearly all of the traffic, so HBM bounds it, or latency for few heads: a CTA has its share
+// of the state's rows in registers, requested before anything else, and the ring rows that the first eight tokens would push
+// out are requested before it is known how many tokens there are.  Few heads are shared by clusters of four CTAs.
 // Tokens are added in order, as single steps would (fp32).
 //
-// The slots that the new tokens take are those that the old ones leave: the cluster meets at a barrier between the last
+// The slots that the new tokens take are those that the old ones leave: the CTAs of a head meet at a barrier between the last
 // read of an old token and the first write of a new one.
 #include "draft_internal.h"
 
@@ -15,7 +16,7 @@ namespace rattn {
 namespace draft {
 namespace {
 
-constexpr int DC_THREADS = 256, DC_CLUSTER = 4, DC_TOKENS = 16;     // tokens whose phi(k), v lie in shared memory at a time
+constexpr int DC_THREADS = 256, DC_TOKENS = DC_THREADS / 32;        // tokens whose phi(k), v lie in shared memory at a time
 
 __device__ __forceinline__ float wmax(float x) {
 #pragma unroll
@@ -28,49 +29,67 @@ __device__ __forceinline__ float wsum(float x) {
   return x;
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(DC_THREADS) draft_commit_kernel(const __grid_constant__ DraftArgs a) {
-  constexpr int C = D / 32, CG = D / 4, LANES = DC_THREADS / CG, ROWS = D / DC_CLUSTER / LANES;
+template <typename T, int D, int CS>
+__global__ void __launch_bounds__(DC_THREADS, CS == 1 ? 2 : 4) draft_commit_kernel(const __grid_constant__ DraftArgs a) {
+  constexpr int C = D / 32, CG = D / 4, LANES = DC_THREADS / CG, ROWS = D / CS / LANES;
   __shared__ __align__(16) float fk[DC_TOKENS][D];
   __shared__ __align__(16) float vo[DC_TOKENS][D];
   __shared__ int path[kMaxNodes];
   __shared__ int n_s;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int z = blockIdx.x / DC_CLUSTER, rank = blockIdx.x % DC_CLUSTER, b = z / a.H_kv, hk = z % a.H_kv;
-  const int c4 = (tid % CG) * 4, row0 = rank * (D / DC_CLUSTER) + tid / CG;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, w = a.w;
+  const int z = blockIdx.x / CS, rank = blockIdx.x % CS, b = z / a.H_kv, hk = z % a.H_kv;
+  const int c4 = (tid % CG) * 4, row0 = rank * (D / CS) + tid / CG;
+  if (tid == 0) n_s = a.N;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");        // the inputs may come from the kernel before
+  const int pos = entry_pos(a, b), n_raw = a.n_accepted[b];
+  const int node = tid < a.N ? a.path[(size_t)b * a.N + tid] : -1;
   float* S = a.state + (size_t)z * D * D;
   float4 acc[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) acc[i] = *reinterpret_cast<const float4*>(S + (size_t)(row0 + i * LANES) * D + c4);
-  if (tid == 0) n_s = min(max(a.n_accepted[b], 0), a.N);
-  __syncthreads();
-  if (tid < a.N) {
-    path[tid] = a.path[(size_t)b * a.N + tid];
-    if (path[tid] < 0 || path[tid] >= a.N) atomicMin(&n_s, tid);
-  }
-  __syncthreads();
-  const int n = n_s, w = a.w, pos = entry_pos(a, b), head = pos % w;
-  if (n == 0) return;                                       // the same for the whole cluster
   T* kr = static_cast<T*>(a.k_ring) + (size_t)z * w * D;
   T* vr = static_cast<T*>(a.v_ring) + (size_t)z * w * D;
   const T* kn = static_cast<const T*>(a.k);
   const T* vn = static_cast<const T*>(a.v);
+  const int head = pos % w, a0 = pos < w ? w - pos : 0;     // a0: the first accepted token that pushes one out
+  // this warp's token of the first eight, where it is one of the ring
+  T k1[C], v1[C];
+  const int at1 = a0 + warp;
+  if (at1 < a.N && at1 < w) {
+    const size_t from = (size_t)((head + at1) % w) * D + lane;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      k1[i] = kr[from + 32 * i];
+      v1[i] = vr[from + 32 * i];
+    }
+  }
+  __syncthreads();
+  if (tid < a.N) {
+    path[tid] = node;
+    if (node < 0 || node >= a.N) atomicMin(&n_s, tid);
+  }
+  __syncthreads();
+  const int n = min(n_s, max(n_raw, 0));
+  if (n == 0) return;                                       // the same for the whole cluster
 
-  const int a0 = pos < w ? w - pos : 0;                     // the first accepted token that pushes one out
   for (int t0 = a0; t0 < n; t0 += DC_TOKENS) {
-    const int m = min(DC_TOKENS, n - t0);
-    for (int t = warp; t < m; t += DC_THREADS / 32) {
-      const int at = t0 + t;
-      const size_t from = at < w ? (size_t)((head + at) % w) * D : node_at(a, b, hk, a.H_kv, path[at - w]);
-      const T* ko = (at < w ? kr : kn) + from;
-      const T* vv = (at < w ? vr : vn) + from;
+    const int m = min(DC_TOKENS, n - t0), at = t0 + warp;
+    if (warp < m) {
+      if (t0 != a0 || at >= w) {
+        const bool ring = at < w;
+        const size_t from = ring ? (size_t)((head + at) % w) * D : node_at(a, b, hk, a.H_kv, path[at - w]);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          k1[i] = ((ring ? kr : kn) + from)[lane + 32 * i];
+          v1[i] = ((ring ? vr : vn) + from)[lane + 32 * i];
+        }
+      }
       float x[C];
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        x[i] = (float)ko[lane + 32 * i];
-        vo[t][lane + 32 * i] = (float)vv[lane + 32 * i];
+        x[i] = (float)k1[i];
+        vo[warp][lane + 32 * i] = (float)v1[i];
       }
       if (a.phi == RATTN_PHI_SOFTMAX) {
         float mx = x[0], s = 0.f;
@@ -87,7 +106,7 @@ __global__ void __launch_bounds__(DC_THREADS) draft_commit_kernel(const __grid_c
         for (int i = 0; i < C; ++i) x[i] = fmaxf(x[i], 0.f);
       }
 #pragma unroll
-      for (int i = 0; i < C; ++i) fk[t][lane + 32 * i] = x[i];
+      for (int i = 0; i < C; ++i) fk[warp][lane + 32 * i] = x[i];
     }
     __syncthreads();
     for (int t = 0; t < m; ++t) {
@@ -104,27 +123,39 @@ __global__ void __launch_bounds__(DC_THREADS) draft_commit_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) *reinterpret_cast<float4*>(S + (size_t)(row0 + i * LANES) * D + c4) = acc[i];
   }
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");    // every old token has been read
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (CS > 1) {                                             // every old token has been read
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
   constexpr int V16 = D * (int)sizeof(T) / 16;              // 16-byte pieces of a row
   const int first = n > w ? n - w : 0;                      // earlier ones have been pushed out by the path itself
   for (int i = tid; i < (n - first) * 2 * V16; i += DC_THREADS) {
     const int t = first + i / (2 * V16), piece = i % V16;
-    if (t % DC_CLUSTER != rank) continue;
+    if (t % CS != rank) continue;
     const bool is_v = (i / V16) & 1;
     const size_t from = node_at(a, b, hk, a.H_kv, path[t]), to = (size_t)((head + (t % w)) % w) * D;
     reinterpret_cast<uint4*>((is_v ? vr : kr) + to)[piece] = reinterpret_cast<const uint4*>((is_v ? vn : kn) + from)[piece];
   }
 }
 
-template <typename T, int D>
-cudaError_t launch_commit_as(const DraftArgs& a, cudaStream_t s) {
+template <typename T, int D, int CS>
+cudaError_t launch_commit_cs(const DraftArgs& a, cudaStream_t s) {
   KernelTimer kt("draft_commit", s);
-  const cudaError_t e = launch_pdl_cluster(draft_commit_kernel<T, D>, dim3((unsigned)(a.B * a.H_kv * DC_CLUSTER)), dim3(DC_THREADS),
-                                           0, s, true, DC_CLUSTER, a);
+  const cudaError_t e = launch_pdl_cluster(draft_commit_kernel<T, D, CS>, dim3((unsigned)(a.B * a.H_kv * CS)), dim3(DC_THREADS), 0, s,
+                                           true, CS, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   return cudaGetLastError();
+}
+
+// A head to a cluster of four CTAs while there are no more heads than SMs, to one CTA beyond (d = 128, bf16; one CTA / four:
+// 8 heads 4.1 / 3.6 us, 128 heads 5.8 / 5.3, 256 heads 6.5 / 9.4, 512 heads 11.2 / 16.9: the state's 67 MB at 5.9 TB/s).
+template <typename T, int D>
+cudaError_t launch_commit_as(const DraftArgs& a, cudaStream_t s) {
+  int n_sm = 0;
+  const cudaError_t e = sm_count(&n_sm);
+  if (e != cudaSuccess) return e;
+  return a.B * a.H_kv <= n_sm ? launch_commit_cs<T, D, 4>(a, s) : launch_commit_cs<T, D, 1>(a, s);
 }
 
 }  // namespace
