@@ -33,6 +33,7 @@ struct AxesFreqs : Freqs {
   unsigned char axis[64];
   const int* at;                      // [n_axes, B, T]
   size_t tokens;                      // B T
+  int n_axes;
 };
 template <bool AXES> struct FreqsOf { using Type = Freqs; };
 template <> struct FreqsOf<true> { using Type = AxesFreqs; };
@@ -63,11 +64,25 @@ __device__ __forceinline__ float reduced(double ang) {
   constexpr double kTwoPi = 6.283185307179586476925286766559;
   return (float)(ang - kTwoPi * rint(ang * (1.0 / kTwoPi)));
 }
-__device__ __forceinline__ float angle(const QkArgs& a, const Freqs& f, int i, int b, int t) {
-  return reduced((double)((a.pos ? (long long)a.pos[b] : a.pos0) + t) * f.inv[i]);
+// Where token t of batch entry b stands: its position, or its coordinates, all of them asked for before one is used.
+struct Place { long long at; };
+struct AxesPlace {
+  int at[4];
+  __device__ __forceinline__ int on(int x) const { return x < 2 ? (x == 0 ? at[0] : at[1]) : (x == 2 ? at[2] : at[3]); }
+};
+__device__ __forceinline__ Place place_of(const QkArgs& a, const Freqs&, int b, int t) {
+  return {(a.pos ? (long long)a.pos[b] : a.pos0) + t};
 }
-__device__ __forceinline__ float angle(const QkArgs& a, const AxesFreqs& f, int i, int b, int t) {
-  return reduced((double)f.at[f.axis[i] * f.tokens + (size_t)b * a.T + t] * f.inv[i]);
+__device__ __forceinline__ AxesPlace place_of(const QkArgs& a, const AxesFreqs& f, int b, int t) {
+  AxesPlace p;
+  const int* at = f.at + (size_t)b * a.T + t;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) p.at[x] = x < f.n_axes ? __ldg(at + x * f.tokens) : 0;
+  return p;
+}
+__device__ __forceinline__ float angle(const Freqs& f, int i, const Place& p) { return reduced((double)p.at * f.inv[i]); }
+__device__ __forceinline__ float angle(const AxesFreqs& f, int i, const AxesPlace& p) {
+  return reduced((double)p.on(f.axis[i]) * f.inv[i]);
 }
 
 template <typename T> struct Io;
@@ -118,10 +133,10 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 
 // cos and sin of the angles of this lane's 8 pairs
-template <typename F>
-__device__ __forceinline__ void rotation(const QkArgs& a, const F& f, int first_pair, int b, int t, float (&c)[8], float (&s)[8]) {
+template <typename F, typename P>
+__device__ __forceinline__ void rotation(const F& f, int first_pair, const P& p, float (&c)[8], float (&s)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) sincosf(angle(a, f, first_pair + j, b, t), &s[j], &c[j]);
+  for (int j = 0; j < 8; ++j) sincosf(angle(f, first_pair + j, p), &s[j], &c[j]);
 }
 
 __device__ __forceinline__ void load_gain(const float* gain, int lo_first, int half, float (&g_lo)[8],
@@ -284,6 +299,7 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ typ
 #pragma unroll
   for (int j = 0; j < 16; ++j) acc[j] = 0.f;
   int cur_which = -1, cur_rb = -1;
+  AxesPlace next_place;                               // [B, H, T, d] with axes: of the next row block
 
   // per-CTA sum of the gain-gradient terms over its rows, in row order, to this CTA's partial row
   auto flush = [&](int which) {
@@ -319,13 +335,33 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ typ
     tbl_first = cx.b0 * a.T + cx.t0;
     const int n_tok = min(small_div(cx.h0 + n - 1, a.inv_H[cx.which]) + 1, a.tbl_tokens);
     tbl_end = tbl_first + n_tok;
-    for (int e = tid; e < n_tok * (D / 2); e += QK_THREADS) {
-      const int tok = e / (D / 2), pair = e % (D / 2);
-      int t = cx.t0 + tok, b = cx.b0;
-      while (t >= a.T) { t -= a.T; ++b; }
-      float sn, cs;
-      sincosf(angle(a, f, pair, b, t), &sn, &cs);
-      tbl[tbl_at(tok, pair)] = make_float2(cs, sn);
+    if constexpr (AXES) {
+      // a thread's entries are all of one pair, and tokens b T + t lie side by side on every axis
+      constexpr int STEP = QK_THREADS / (D / 2), AHEAD = 4;
+      const int pair = tid % (D / 2);
+      const int* at = f.at + f.axis[pair] * f.tokens + tbl_first;
+      const double inv = f.inv[pair];
+      for (int tok = tid / (D / 2); tok < n_tok; tok += STEP * AHEAD) {
+        int x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) x[j] = __ldg(at + min(tok + j * STEP, n_tok - 1));
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+          if (tok + j * STEP < n_tok) {
+            float sn, cs;
+            sincosf(reduced((double)x[j] * inv), &sn, &cs);
+            tbl[tbl_at(tok + j * STEP, pair)] = make_float2(cs, sn);
+          }
+      }
+    } else {
+      for (int e = tid; e < n_tok * (D / 2); e += QK_THREADS) {
+        const int tok = e / (D / 2), pair = e % (D / 2);
+        int t = cx.t0 + tok, b = cx.b0;
+        while (t >= a.T) { t -= a.T; ++b; }
+        float sn, cs;
+        sincosf(angle(f, pair, place_of(a, f, b, t)), &sn, &cs);
+        tbl[tbl_at(tok, pair)] = make_float2(cs, sn);
+      }
     }
   };
   Cursor ch = cursor_at<RPB>(a, lo);
@@ -358,8 +394,15 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ typ
     if (!BTHD) {
       const int rb = ch.b * a.nblk_t + ch.tb;
       if (rb != cur_rb && a.rotate) {
-        // (rows behind the last token have no coordinates to be read)
-        rotation(a, f, 8 * l, ch.b, AXES ? min(ch.tb * RPB + row, a.T - 1) : ch.tb * RPB + row, c, s);
+        // Coordinates are asked for a row block ahead (rows behind the last token have none to be read).
+        if constexpr (AXES) {
+          auto at = [&](int b, int tb) { return place_of(a, f, b, min(tb * RPB + row, a.T - 1)); };
+          rotation(f, 8 * l, cur_rb < 0 ? at(ch.b, ch.tb) : next_place, c, s);
+          const bool wrap = ch.tb + 1 == a.nblk_t;
+          next_place = at(wrap ? (ch.b + 1 == a.B ? 0 : ch.b + 1) : ch.b, wrap ? 0 : ch.tb + 1);
+        } else {
+          rotation(f, 8 * l, place_of(a, f, ch.b, ch.tb * RPB + row), c, s);
+        }
         cur_rb = rb;
       }
     } else if (tabled) {
@@ -506,11 +549,12 @@ __global__ void __launch_bounds__(QK_THREADS) qk_small_kernel(const __grid_const
     g_hi[j] = gain ? gain[D / 2 + i0 + j] : 1.f;
   }
   float c[PPL], s[PPL];
+  const auto place = place_of(a, f, b, t);
 #pragma unroll
   for (int j = 0; j < PPL; ++j) {
     c[j] = 1.f;
     s[j] = 0.f;
-    if (a.rotate) sincosf(angle(a, f, i0 + j, b, t), &s[j], &c[j]);
+    if (a.rotate) sincosf(angle(f, i0 + j, place), &s[j], &c[j]);
   }
 #pragma unroll
   for (int j = 0; j < PPL; ++j) ss += lo[j] * lo[j] + hi[j] * hi[j];
@@ -741,6 +785,7 @@ void fill_axes(const rattn_qk_params* p, const rattn_qk_axes* x, AxesFreqs* f) {
   *f = known.f;
   f->at = x->at;
   f->tokens = (size_t)p->B * p->T;
+  f->n_axes = x->n_axes;
 }
 
 template <bool AXES>
