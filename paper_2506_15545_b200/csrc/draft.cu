@@ -57,15 +57,15 @@ template <> struct Vec<__nv_bfloat16> {
 
 template <typename T, int D>
 __device__ __forceinline__ float dot(const float* q, const T* k) {
-  float s = 0.f;
-#pragma unroll 4
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 16
   for (int i = 0; i < D; i += Vec<T>::N) {
     float x[Vec<T>::N];
     Vec<T>::load(k + i, x);
 #pragma unroll
-    for (int j = 0; j < Vec<T>::N; ++j) s += q[i + j] * x[j];
+    for (int j = 0; j < Vec<T>::N; ++j) s[j & 3] += q[i + j] * x[j];
   }
-  return s;
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 // phi(q) . phi(k), fq = phi(q)
@@ -158,6 +158,22 @@ __global__ void __launch_bounds__(DG_WARPS * 32) draft_generic_kernel(const __gr
       l += wsum(p);
     }
     if (far) p = phi_dot<T, D>(f_s[warp], kb + lane * stride, a.phi);
+    if (nears == 0xffffffffu) {                              // all of them near: eight values on their way at a time
+      for (int j0 = 0; j0 < 32; j0 += 8) {
+        T vv[8][C];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int i = 0; i < C; ++i) vv[j][i] = vb[(j0 + j) * stride + lane + 32 * i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float pj = __shfl_sync(0xffffffffu, p, j0 + j);
+#pragma unroll
+          for (int i = 0; i < C; ++i) o[i] += pj * (float)vv[j][i];
+        }
+      }
+      return;
+    }
     for (uint32_t todo = nears | fars; todo; todo &= todo - 1) {
       const int j = __ffs(todo) - 1;
       const float pj = __shfl_sync(0xffffffffu, p, j);
@@ -185,7 +201,7 @@ __global__ void __launch_bounds__(DG_WARPS * 32) draft_generic_kernel(const __gr
     block(static_cast<const T*>(a.k) + at, static_cast<const T*>(a.v) + at, step, near, mine && !near);
   }
   const float* S = a.state + (size_t)z * D * D;
-#pragma unroll 4
+#pragma unroll 16
   for (int f = 0; f < D; ++f) {
     const float fq = f_s[warp][f];
 #pragma unroll
