@@ -359,8 +359,78 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   // features), leading parts and remainders.
   const uint32_t sQ = smem_u32(smem);
   const int k0 = 8 * rank / CS, k1 = 8 * (rank + 1) / CS;    // this CTA's steps of 16 features
+  const int h0 = k0 >> 2;                                    // the (first) half that they lie in
   const float* S = d.state + (size_t)it.z * TILE * TILE;
   float4 x_s[16];
+  // phi(Q), while the last products run: every score has been formed, and every slot but those of the last two V tiles is free.
+  // Leading parts go over Q, without the normalisation (inv_phi of the row's thread), remainders to the first two spare slots.
+  // All four row warps: a row's thread takes all 16 pieces of eight features, or, where one or two warps have rows, two or four
+  // threads in different warps share them.  (Loops that run once per row stay rolled: unrolled, they take as long as their
+  // instructions take to arrive.  One thread per row took 4.4k cycles.)
+  auto map_q = [&]() {
+    const int row_warps = (it.rows + 31) >> 5, share = row_warps == 1 ? 4 : row_warps == 2 ? 2 : 1;      // threads per row
+    const int r = share == 1 ? tid : lane + 32 * (warp % row_warps), part = share == 1 ? 0 : warp / row_warps;
+    if (share == 1 && 32 * warp >= it.rows) return;          // (whole warps: rows behind the last are zero and mapped along)
+    mbar_wait(&bars->q_full, 0u, &bars->abort);
+    if (it.nt > 0 && part > 0) mbar_wait(&bars->scored, 0u, &bars->abort);        // (the row's own thread has seen the last scores)
+    const int n = 16 / share, c0 = part * n, sw = r & 7;
+    unsigned char* row = smem + r * 128;
+    // [2][4][32 or 64]: maxima and sums of the threads that share a row, where the rows behind the last would have their remainders
+    float* ex = reinterpret_cast<float*>(spare(0) + 64 * 128);
+    float mq = 0.f, sq = 0.f;
+    if (d.phi == RATTN_PHI_SOFTMAX) {
+      mq = -INFINITY;
+#pragma unroll 2
+      for (int c = c0; c < c0 + n; ++c) {
+        const uint4 u = *reinterpret_cast<const uint4*>(row + (c >> 3) * HALF_BYTES + (((c & 7) ^ sw) << 4));
+        const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mq = fmaxf(mq, fmaxf(__uint_as_float(w4[i] << 16), __uint_as_float(w4[i] & 0xffff0000u)));
+      }
+      if (share > 1) ex[part * 64 + r] = mq;
+    }
+    if (share > 1) {
+      __syncwarp();
+      named_sync(3, 128);
+      if (d.phi == RATTN_PHI_SOFTMAX)
+        for (int i = 0; i < share; ++i) mq = fmaxf(mq, ex[i * 64 + r]);
+    }
+    mq *= LOG2E;
+    unsigned char* lo_row = spare(0) + r * 128;
+    const ptrdiff_t lo_step = spare(1) - spare(0);
+#pragma unroll 2
+    for (int c = c0; c < c0 + n; ++c) {
+      const int at = ((c & 7) ^ sw) << 4;
+      uint4* p16 = reinterpret_cast<uint4*>(row + (c >> 3) * HALF_BYTES + at);
+      const uint4 u = *p16;
+      const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float p = __uint_as_float(w4[i] << 16), q = __uint_as_float(w4[i] & 0xffff0000u);
+        if (d.phi == RATTN_PHI_SOFTMAX) {
+          p = ex2(p * LOG2E - mq);
+          q = ex2(q * LOG2E - mq);
+          sq += p + q;
+        } else if (d.phi == RATTN_PHI_RELU) {
+          p = fmaxf(p, 0.f);
+          q = fmaxf(q, 0.f);
+        }
+        split2(p, q, &hi[i], &lo[i]);
+      }
+      *p16 = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(lo_row + (c >> 3) * lo_step + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    fence_proxy_async_smem();
+    if (share > 1) {
+      ex[256 + part * 64 + r] = sq;
+      __syncwarp();
+      named_sync(3, 128);
+      sq = 0.f;
+      for (int i = 0; i < share; ++i) sq += ex[256 + i * 64 + r];
+    }
+    if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
+  };
   // 16 float4 of S per thread (128 threads), then their two halves to the last two spare slots
   auto load_s = [&](int hh, float4 (&x)[16]) {
     const int c = tid - 128;
@@ -519,51 +589,9 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         tc_fence_before();
         mbar_arrive(&bars->p_ready[t & 1]);
       }
-      mbar_wait(&bars->q_full, 0u, &bars->abort);
-      // phi(Q), while the last products run: every score has been formed and every slot but those of the last two V tiles is
-        // free.  Leading parts go over Q, remainders to the next two slots.
-      // (Loops that run once per row stay rolled: unrolled, they take as long as their instructions take to arrive.)
-      float mq = 0.f, sq = 0.f;
-      const unsigned char* q_row = smem + tid * 128;
-      const int sw = tid & 7;
-      if (d.phi == RATTN_PHI_SOFTMAX) {
-        mq = -INFINITY;
-#pragma unroll 2
-        for (int c = 0; c < 16; ++c) {
-          const uint4 u = *reinterpret_cast<const uint4*>(q_row + (c >> 3) * HALF_BYTES + (((c & 7) ^ sw) << 4));
-          const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mq = fmaxf(mq, fmaxf(__uint_as_float(w4[i] << 16), __uint_as_float(w4[i] & 0xffff0000u)));
-        }
-        mq *= LOG2E;
-      }
-      unsigned char* lo_row = spare(0) + tid * 128;
-      const ptrdiff_t lo_step = spare(1) - spare(0);
-#pragma unroll 2
-      for (int c = 0; c < 16; ++c) {
-        const int at = ((c & 7) ^ sw) << 4;
-        uint4* p16 = reinterpret_cast<uint4*>(smem + tid * 128 + (c >> 3) * HALF_BYTES + at);
-        const uint4 u = *p16;
-        const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float p = __uint_as_float(w4[i] << 16), q = __uint_as_float(w4[i] & 0xffff0000u);
-          if (d.phi == RATTN_PHI_SOFTMAX) {
-            p = ex2(p * LOG2E - mq);
-            q = ex2(q * LOG2E - mq);
-            sq += p + q;
-          } else if (d.phi == RATTN_PHI_RELU) {
-            p = fmaxf(p, 0.f);
-            q = fmaxf(q, 0.f);
-          }
-          split2(p, q, &hi[i], &lo[i]);
-        }
-        *p16 = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(lo_row + (c >> 3) * lo_step + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-      }
-      if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
-      fence_proxy_async_smem();
+    }
+    map_q();
+    if (32 * warp < it.rows) {
       // (a barrier of its own: by now pv_done may be one or two phases on)
       if (it.nt > 0) mbar_wait(&bars->o_full, 0u, &bars->abort);
       tc_fence_after();
@@ -576,7 +604,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 #endif
   } else if (warp == 5) {
     window_load(maps, it, smem, bars);
-    load_s(0, x_s);
+    load_s(h0, x_s);
   } else {
     window_clean(d, it, smem, bars, tid - 192);
     // nodes that some row has more than w levels up; the far keys, as soon as there is room for them
@@ -590,7 +618,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     mbar_wait(&bars->scored, 0u, &bars->abort);
     __syncwarp();
     if (rank == 0) build_k(0, corner + bars->n_far_node, 6, 2);
-    load_s(0, x_s);
+    load_s(h0, x_s);
   }
   __syncthreads();                       // the window's products are complete, its slots free, all nodes looked at
   tc_fence_after();
@@ -703,21 +731,22 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 
   else if (warp >= 4) {
     // phi(Q) S meanwhile, half of the features after the other
-    if (warp == 4) load_s(0, x_s);
+    if (warp == 4) load_s(h0, x_s);
     bool acc = false;
 #pragma unroll 1
-    for (int hh = 0; hh < 2; ++hh) {
-      if (hh == 1) {
+    for (int hh = h0; hh < 2; ++hh) {
+      if (hh > h0) {
+        if (CL) break;                                       // (the CTAs of a cluster have features of one half each)
         mbar_wait(&bars->done, 0u, &bars->abort);
         __syncwarp();
       }
       store_s(x_s);
-      if (hh == 0) load_s(1, x_s);
+      if (!CL && hh == 0) load_s(1, x_s);
       named_sync(2, 128);
       if (warp == 4) {
         tc_fence_after();
         acc = mma_state(hh, acc);
-        if (hh == 0) mma_commit(&bars->done);
+        if (!CL && hh == 0) mma_commit(&bars->done);
       }
     }
     load_v(0, v_far);
@@ -725,12 +754,12 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  uint32_t done_phase = 1;
+  uint32_t done_phase = CL ? 0 : 1;
   if (warp == 4) {
     if (n_far > 0) mma_far_scores(0);
     mma_commit(&bars->done);
   }
-  mbar_wait(&bars->done, 1u, &bars->abort);
+  mbar_wait(&bars->done, done_phase & 1u, &bars->abort);
   __syncwarp();
   tc_fence_after();
   if (n_far > 0) {                                           // (the same for all threads)
@@ -792,13 +821,32 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       tc_fence_before();
     }
     __syncthreads();
+    const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+    const int c0 = 4 * lane;
+    float4 gs = one, gr = one;
+    auto gains = [&](int r) {
+      if (r >= it.rows) return;
+      const int n = small_div(it.row0 + r, a.inv_group);
+      const size_t at = (size_t)(it.hk * G + it.row0 + r - n * G) * TILE + c0;
+      if (d.gamma_swa) gs = *reinterpret_cast<const float4*>(d.gamma_swa + at);
+      if (d.gamma_rla) gr = *reinterpret_cast<const float4*>(d.gamma_rla + at);
+    };
+    gains(rank + CS * warp);                                 // (on their way while the cluster meets)
     cluster_arrive();                                        // partial outputs of every CTA are in place
     cluster_wait();
     // a wait that ran out in one of the CTAs ends the call for all of them
     const bool ok = !__any_sync(0xffffffffu, lane < CS && __float_as_uint(ld_cluster(cluster_addr(&bars->abort, lane))) != 0u);
     for (int r = rank + CS * warp; ok && r < it.rows; r += CS * (DA_THREADS / 32)) {
-      const int n = small_div(it.row0 + r, a.inv_group), h = it.hk * G + it.row0 + r - n * G, c0 = 4 * lane;
+      const int n = small_div(it.row0 + r, a.inv_group), h = it.hk * G + it.row0 + r - n * G;
+      if (r >= CS * (DA_THREADS / 32)) gains(r);
       if (bars->depth[n] < 0) continue;
+      float4 p[8], q[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < CS) {
+          p[k] = ld_cluster4(cluster_addr(smem + DA_OFF_OX + at_ox(r, lane), k));
+          q[k] = ld_cluster4(cluster_addr(smem + DA_OFF_OX + DA_CLUSTER_ROWS * 512 + at_ox(r, lane), k));
+        }
       float m_r = -INFINITY, l_r = 0.f;
       if (lane < CS) {
         m_r = ld_cluster(cluster_addr(stat + r, lane));
@@ -807,13 +855,6 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       const float m = wmax(m_r), f = ex2(m_r - (m == -INFINITY ? 0.f : m));
       const float inv = 1.f / wsum(lane < CS ? f * l_r : 0.f);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-      float4 p[8], q[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < CS) {
-          p[k] = ld_cluster4(cluster_addr(smem + DA_OFF_OX + at_ox(r, lane), k));
-          q[k] = ld_cluster4(cluster_addr(smem + DA_OFF_OX + DA_CLUSTER_ROWS * 512 + at_ox(r, lane), k));
-        }
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         if (k < CS) {
@@ -823,9 +864,6 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         }
       const float ss = wsum(x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w), sr = wsum(y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w);
       const float is = rsqrtf(ss / TILE + d.eps), ir = rsqrtf(sr / TILE + d.eps);
-      const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-      const float4 gs = d.gamma_swa ? *reinterpret_cast<const float4*>(d.gamma_swa + (size_t)h * TILE + c0) : one;
-      const float4 gr = d.gamma_rla ? *reinterpret_cast<const float4*>(d.gamma_rla + (size_t)h * TILE + c0) : one;
       *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
           make_uint2(pack_bf16(gs.x * x.x * is + gr.x * y.x * ir, gs.y * x.y * is + gr.y * y.y * ir),
                      pack_bf16(gs.z * x.z * is + gr.z * y.z * ir, gs.w * x.w * is + gr.w * y.w * ir));
