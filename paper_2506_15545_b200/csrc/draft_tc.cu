@@ -5,9 +5,10 @@
 //
 //   4 row warps   (thread = row = TMEM lane) online softmax straight out of TMEM; the weights go back over their scores as a
 //                 bf16 pair, leading part and remainder, and P V runs over both: 16 bits of every weight, no restriction on v
-//   MMA warp      S = Q K^T, O += P V (A operand from TMEM), then the linear branch's products
+//   score warp    S = Q K^T
+//   MMA warp      O += P V (A operand from TMEM), then the linear branch's products
 //   loader warp   TMA: K and V tiles through a ring of five 16 KB slots
-//   2 helper warps  clear V rows that belong to no token or node (0 * NaN), and find nodes whose values are not finite
+//   helper warp   clears V rows that belong to no token or node (0 * NaN), and finds nodes whose values are not finite
 //
 // Masks: a row at depth e does not see the e oldest slots (as intervals of slots, in the tiles that hold some of them) and
 // sees the nodes of its own path (128 bits, from a walk up its parents).
@@ -48,7 +49,7 @@ constexpr float PARK = 32767.f / 11.32f;                     // steps per unit o
 __device__ int g_draft_status;           // RATTN_ERR_TIMEOUT once a bounded wait has expired
 
 struct Bars {
-  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], q_full, pv_done, scored, o_full, done, drain;
+  uint64_t full[DA_NS], free_[DA_NS], s_full[2], p_ready[2], pv_done[2], q_full, scored, o_full, done, drain;
   // The (at most three) V tiles that are cleaned: landed, cleaned.  Their landing has barriers of its own, because the
   // helpers follow these uses of the slots alone and a wait by parity cannot skip a phase.
   uint64_t landed[3], clean[3];
@@ -111,11 +112,14 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t a) {
   return v;
 }
 
-// two floats as a bf16 pair word, and the remainders as another
+// Two floats as a word of leading parts (the upper halves of their bits, a byte permutation instead of a conversion) and one
+// of remainders, which a conversion rounds: off by 2^-16 of the value at most.
 __device__ __forceinline__ void split2(float a, float b, uint32_t* hi, uint32_t* lo) {
-  const uint32_t h = pack_bf16(a, b);
-  *hi = h;
-  *lo = pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u));
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  *hi = __byte_perm(x, y, 0x7632);
+  const float2 r = __ffma2_rn(make_float2(__uint_as_float(x & 0xffff0000u), __uint_as_float(y & 0xffff0000u)), make_float2(-1.f, -1.f),
+                              make_float2(a, b));
+  *lo = pack_bf16(r.x, r.y);
 }
 // byte offset of 16-byte chunk c (0 .. 15) of row r in a [128 x 128] bf16 tile (two swizzled halves), and in a half tile
 __device__ __forceinline__ uint32_t at_tile(int r, int c) { return (uint32_t)((c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
@@ -188,34 +192,33 @@ __device__ __forceinline__ void mma_weights(uint32_t o, uint32_t p, uint32_t v, 
 
 // ---------------------------------------------------------------------------------------------- window loop, by role
 
-__device__ void window_mma(const Item& it, unsigned char* smem, Bars* bars, uint32_t tS, uint32_t tO) {
+// Scores and products are issued by two warps: with its waits (some 300 cycles each, satisfied or not), its issue slots (65 per
+// instruction) and its commits one warp took 2.1 - 2.4k cycles a tile, the row warps take 1.5k.
+__device__ void window_scores(const Item& it, unsigned char* smem, Bars* bars, uint32_t tS) {
   const uint32_t sQ = smem_u32(smem), sR = sQ + DA_OFF_RING;
-  auto scores = [&](int t) {
+  mbar_wait_warp(&bars->q_full, 0u, &bars->abort);
+  for (int t = 0; t < it.nt; ++t) {
     const int i = use_k(t), slot = i % DA_NS;
+    mbar_wait_warp(&bars->full[slot], (uint32_t)(i / DA_NS) & 1u, &bars->abort);
+    if (t >= 2) mbar_wait_warp(&bars->pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, &bars->abort);     // its weights lay there
+    tc_fence_after();
     mma_scores(tS + 64 * (t & 1), sQ, sR + slot * HT_BYTES);
     mma_commit(&bars->s_full[t & 1]);
     mma_commit(&bars->free_[slot]);
-  };
-  auto wait_use = [&](int i) { mbar_wait_warp(&bars->full[i % DA_NS], (uint32_t)(i / DA_NS) & 1u, &bars->abort); };
-  mbar_wait_warp(&bars->q_full, 0u, &bars->abort);
-  for (int t = 0; t < 2 && t < it.nt; ++t) {
-    wait_use(use_k(t));
-    tc_fence_after();
-    scores(t);
   }
-  if (it.nt <= 2) mma_commit(&bars->scored);                 // the last scores have gone out
+  mma_commit(&bars->scored);
+}
+__device__ void window_products(const Item& it, unsigned char* smem, Bars* bars, uint32_t tS, uint32_t tO) {
+  const uint32_t sR = smem_u32(smem) + DA_OFF_RING;
   for (int t = 0; t < it.nt; ++t) {
     const int i = use_v(t, it.nt), slot = i % DA_NS;
     if (needs_cleaning(it, it.t0 + t)) mbar_wait_warp(&bars->clean[it.t0 + t - first_unclean(it)], 0u, &bars->abort);
-    else wait_use(i);
-    if (t + 2 < it.nt) wait_use(use_k(t + 2));
+    else mbar_wait_warp(&bars->full[slot], (uint32_t)(i / DA_NS) & 1u, &bars->abort);
     mbar_wait_warp(&bars->p_ready[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
     tc_fence_after();
     mma_weights(tO, tS + 64 * (t & 1), sR + slot * HT_BYTES, t > 0, 4);
-    mma_commit(t + 1 < it.nt ? &bars->pv_done : &bars->o_full);
-    mma_commit(&bars->free_[slot]);
-    if (t + 2 < it.nt) scores(t + 2);
-    if (t + 3 == it.nt) mma_commit(&bars->scored);
+    mma_commit(&bars->pv_done[t & 1]);
+    mma_commit(t + 1 < it.nt ? &bars->free_[slot] : &bars->o_full);      // (nothing follows into the last one's slot)
   }
 }
 
@@ -232,10 +235,11 @@ __device__ void window_clean(const DraftArgs& d, const Item& it, unsigned char* 
     mbar_wait(&bars->landed[n], 0u, &bars->abort);
     unsigned char* tile = smem + DA_OFF_RING + slot * HT_BYTES;
     if (T < it.n_ring) {
-      for (int c = cid + (it.held & 63) * 16; c < 64 * 16; c += 64) *reinterpret_cast<uint4*>(tile + at_half(c >> 4, c & 15)) = make_uint4(0u, 0u, 0u, 0u);
+      for (int c = cid + (it.held & 63) * 16; c < 64 * 16; c += 32) *reinterpret_cast<uint4*>(tile + at_half(c >> 4, c & 15)) = make_uint4(0u, 0u, 0u, 0u);
     } else {
       const int n0 = 64 * (T - it.n_ring);
-      for (int c = cid; c < 64 * 16; c += 64) {
+#pragma unroll 4
+      for (int c = cid; c < 64 * 16; c += 32) {
         uint4* p = reinterpret_cast<uint4*>(tile + at_half(c >> 4, c & 15));
         const int j = n0 + (c >> 4);
         const uint4 x = *p;
@@ -267,18 +271,18 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars->s_full[i], 1);
+      mbar_init(&bars->pv_done[i], 1);
       mbar_init(&bars->p_ready[i], (uint32_t)((rows + 31) & ~31));      // the warps that have rows
     }
     mbar_init(&bars->q_full, 128);
-    mbar_init(&bars->pv_done, 1);
     for (int i = 0; i < 3; ++i) {
       mbar_init(&bars->landed[i], 1);
-      mbar_init(&bars->clean[i], 64);
+      mbar_init(&bars->clean[i], 32);
     }
     mbar_init(&bars->scored, 1);
     mbar_init(&bars->o_full, 1);
     mbar_init(&bars->done, 1);
-    mbar_init(&bars->drain, 1);
+    mbar_init(&bars->drain, 2);
     bars->abort = 0;
     for (int i = 0; i < kMaxNodes / 32; ++i) bars->bad[i] = 0u;
     bars->n_far_node = bars->deepest = 0;
@@ -332,7 +336,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     const int c = tid & 15;
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(d.q) + node_at(d, it.b, it.hk * G, d.H_q, 0) + 8 * c;
     const size_t head = d.layout == RATTN_LAYOUT_BHTD ? (size_t)d.N * TILE : TILE, step = d.layout == RATTN_LAYOUT_BHTD ? TILE : (size_t)d.H_q * TILE;
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < 16; ++i) {
       const int r = (tid >> 4) + 8 * i, row = it.row0 + min(r, it.rows - 1), n = small_div(row, a.inv_group);
       copy16_async(smem_u32(smem + at_tile(r, c)), q + (row - n * G) * head + n * step, r < it.rows);
@@ -477,7 +481,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     return static_cast<const __nv_bfloat16*>(is_v ? d.v : d.k) + node_at(d, it.b, it.hk, d.H_kv, bars->far_node[i - corner]);
   };
   auto build_k = [&](int chunk, int n_far, int first_warp, int n_warps) {
-#pragma unroll 2
+#pragma unroll 1
     for (int i = warp - first_warp; i < FAR && chunk + i < n_far; i += n_warps) {
       const uint2 u = reinterpret_cast<const uint2*>(far_source(chunk + i, false))[lane];
       float x[4] = {__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
@@ -550,7 +554,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
           const float m_new = fmaxf(m_ref, mx);
           if (t > 0) {
             const float f = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
-            mbar_wait(&bars->pv_done, (uint32_t)(t - 1) & 1u, &bars->abort);
+            mbar_wait(&bars->pv_done[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1u, &bars->abort);
             tc_fence_after();
             __syncwarp();
 #pragma unroll 1
@@ -592,13 +596,12 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
     map_q();
     if (32 * warp < it.rows) {
-      // (a barrier of its own: by now pv_done may be one or two phases on)
       if (it.nt > 0) mbar_wait(&bars->o_full, 0u, &bars->abort);
       tc_fence_after();
       __syncwarp();
     }
   } else if (warp == 4) {
-    window_mma(it, smem, bars, tS, tO);
+    window_products(it, smem, bars, tS, tO);
 #ifdef RATTN_DEBUG_KNOBS
     if (a.debug_wait == 2 && rank == CS - 1) bars->abort = 1;     // as if one of its waits had run out
 #endif
@@ -606,7 +609,8 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     window_load(maps, it, smem, bars);
     load_s(h0, x_s);
   } else {
-    window_clean(d, it, smem, bars, tid - 192);
+    if (warp == 6) window_clean(d, it, smem, bars, lane);
+    else window_scores(it, smem, bars, tS);
     // nodes that some row has more than w levels up; the far keys, as soon as there is room for them
     if (dmax > d.w && tid == 192) {
       int n = 0;
@@ -749,48 +753,34 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         if (!CL && hh == 0) mma_commit(&bars->done);
       }
     }
-    load_v(0, v_far);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Far keys, 32 at a time (the first of them are mapped already).  The first commit also covers the products above.  (One copy of
+  // this code, whatever their number: what a CTA executes once it has to wait for.)
   uint32_t done_phase = CL ? 0 : 1;
-  if (warp == 4) {
-    if (n_far > 0) mma_far_scores(0);
-    mma_commit(&bars->done);
-  }
-  mbar_wait(&bars->done, done_phase & 1u, &bars->abort);
-  __syncwarp();
-  tc_fence_after();
-  if (n_far > 0) {                                           // (the same for all threads)
-    if (warp >= 4) store_v(v_far);
-    else if (row_warp) far_weights(0);
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    if (warp == 4) {
-      mma_weights(tS, tO + 64, smem_u32(spare(2)), true, steps_of(0));
-      mma_commit(&bars->done);
-    }
-    mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
+  auto wait_done = [&]() {
+    mbar_wait(&bars->done, done_phase++ & 1u, &bars->abort);
     __syncwarp();
     tc_fence_after();
-  }
-  for (int chunk = FAR; chunk < n_far; chunk += FAR) {       // trees deep enough for more of them (the same for all threads)
-    if (warp >= 4) {
-      build_k(chunk, n_far, 4, 4);
-      load_v(chunk, v_far);
+  };
+  int chunk = 0;
+#pragma unroll 1
+  do {
+    if (chunk > 0) {
+      if (warp >= 4) build_k(chunk, n_far, 4, 4);
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
     if (warp == 4) {
-      mma_far_scores(chunk);
+      if (n_far > 0) mma_far_scores(chunk);
       mma_commit(&bars->done);
     }
-    mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
-    __syncwarp();
-    tc_fence_after();
+    if (warp >= 4) load_v(chunk, v_far);
+    wait_done();
+    if (n_far == 0) break;                                   // (the same for all threads)
     if (warp >= 4) store_v(v_far);
     else if (row_warp) far_weights(chunk);
     tc_fence_before();
@@ -800,10 +790,9 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       mma_weights(tS, tO + 64, smem_u32(spare(2)), true, steps_of(chunk));
       mma_commit(&bars->done);
     }
-    mbar_wait(&bars->done, ++done_phase & 1u, &bars->abort);
-    __syncwarp();
-    tc_fence_after();
-  }
+    wait_done();
+    chunk += FAR;
+  } while (chunk < n_far);
 
   // ---- Section 3.2: two RMS norms and the sum ------------------------------------------------------------------------
   if (CL) {
@@ -934,6 +923,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   }
   if (*(volatile int*)&bars->abort) {
     // a wait ran out: what is still in flight gets a bounded time to land before the memory goes away
+    if (warp == 7) mma_commit(&bars->drain);
     if (warp == 4) {
       mma_commit(&bars->drain);
       for (int i = 0; i < kWaitPolls && !mbar_try_wait(&bars->drain, 0u); ++i) {}
