@@ -365,7 +365,6 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   const int k0 = 8 * rank / CS, k1 = 8 * (rank + 1) / CS;    // this CTA's steps of 16 features
   const int h0 = k0 >> 2;                                    // the (first) half that they lie in
   const float* S = d.state + (size_t)it.z * TILE * TILE;
-  float4 x_s[16];
   // phi(Q), while the last products run: every score has been formed, and every slot but those of the last two V tiles is free.
   // Leading parts go over Q, without the normalisation (inv_phi of the row's thread), remainders to the first two spare slots.
   // All four row warps: a row's thread takes all 16 pieces of eight features, or, where one or two warps have rows, two or four
@@ -435,27 +434,30 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
     if (d.phi == RATTN_PHI_SOFTMAX) inv_phi = 1.f / sq;
   };
-  // 16 float4 of S per thread (128 threads), then their two halves to the last two spare slots
-  auto load_s = [&](int hh, float4 (&x)[16]) {
+  // Half of S (128 threads, 16 float4 each), split, to the last two spare slots.  A CTA of many loads its second half and keeps it
+  // while the first is multiplied; in a cluster there is one half, of which each CTA has a part, and eight loads at a time are
+  // the smaller code (a chain of 6 for one sequence: 12.9 against 13.6 us; elsewhere 4 % slower).
+  constexpr int S_AHEAD = CL ? 8 : 16;
+  float4 x_s[S_AHEAD];
+  auto load_s = [&](int hh, int i0) {
     const int c = tid - 128;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int f = 64 * hh + (c >> 5) + 4 * i;
-      x[i] = f >= 16 * k0 && f < 16 * k1 ? *reinterpret_cast<const float4*>(S + (size_t)f * TILE + (c & 31) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < S_AHEAD; ++i) {
+      const int f = 64 * hh + (c >> 5) + 4 * (i0 + i);
+      x_s[i] = f >= 16 * k0 && f < 16 * k1 ? *reinterpret_cast<const float4*>(S + (size_t)f * TILE + (c & 31) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
   };
-  auto store_s = [&](const float4 (&x)[16]) {
+  auto store_s = [&](int i0) {
     const int c = tid - 128;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < S_AHEAD; ++i) {
       uint2 hi, lo;
-      split2(x[i].x, x[i].y, &hi.x, &lo.x);
-      split2(x[i].z, x[i].w, &hi.y, &lo.y);
-      const uint32_t at = at_half((c >> 5) + 4 * i, (c & 31) >> 1) + (c & 1) * 8;
+      split2(x_s[i].x, x_s[i].y, &hi.x, &lo.x);
+      split2(x_s[i].z, x_s[i].w, &hi.y, &lo.y);
+      const uint32_t at = at_half((c >> 5) + 4 * (i0 + i), (c & 31) >> 1) + (c & 1) * 8;
       *reinterpret_cast<uint2*>(spare(3) + at) = hi;
       *reinterpret_cast<uint2*>(spare(4) + at) = lo;
     }
-    fence_proxy_async_smem();
   };
   // products of the features 64 hh .. 64 hh + 63 with this CTA's part of S (MMA warp)
   auto mma_state = [&](int hh, bool acc) {
@@ -607,7 +609,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 #endif
   } else if (warp == 5) {
     window_load(maps, it, smem, bars);
-    load_s(h0, x_s);
+    if (!CL) load_s(0, 0);
   } else {
     if (warp == 6) window_clean(d, it, smem, bars, lane);
     else window_scores(it, smem, bars, tS);
@@ -622,7 +624,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     mbar_wait(&bars->scored, 0u, &bars->abort);
     __syncwarp();
     if (rank == 0) build_k(0, corner + bars->n_far_node, 6, 2);
-    load_s(h0, x_s);
+    if (!CL) load_s(0, 0);
   }
   __syncthreads();                       // the window's products are complete, its slots free, all nodes looked at
   tc_fence_after();
@@ -735,7 +737,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 
   else if (warp >= 4) {
     // phi(Q) S meanwhile, half of the features after the other
-    if (warp == 4) load_s(h0, x_s);
+    if (!CL && warp == 4) load_s(0, 0);
     bool acc = false;
 #pragma unroll 1
     for (int hh = h0; hh < 2; ++hh) {
@@ -744,8 +746,17 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         mbar_wait(&bars->done, 0u, &bars->abort);
         __syncwarp();
       }
-      store_s(x_s);
-      if (!CL && hh == 0) load_s(1, x_s);
+      if (CL) {
+#pragma unroll 1
+        for (int i0 = 0; i0 < 16; i0 += S_AHEAD) {
+          load_s(hh, i0);
+          store_s(i0);
+        }
+      } else {
+        store_s(0);
+      }
+      fence_proxy_async_smem();
+      if (!CL && hh == 0) load_s(1, 0);
       named_sync(2, 128);
       if (warp == 4) {
         tc_fence_after();
