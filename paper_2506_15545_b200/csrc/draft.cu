@@ -10,9 +10,11 @@
 // near, the others far.  S holds everything older and is shared by all nodes: what a sequential decode would have folded
 // into it along the path is added in quadratic form (at most as many tokens as the tree is deep).
 //
-// The portable kernel gives a warp one row.  Blocks of 32 keys: a lane forms the score of its key, then the lanes hold the
-// features and add the values of those keys that the row sees, one by one -- what it does not see is not read into a product,
-// so NaN or infinity there stays there.
+// The portable kernel: four warps walk tiles of 32 keys, which they load together into shared memory, a warp for one or four rows.
+// A lane forms the scores of its key for the warp's rows, then the lanes hold the features and add the values of those keys that a row
+// sees, one by one -- what it does not see is not multiplied, so NaN or infinity there stays there.  It is bound by its
+// shared-memory loads and the latency of a tile (16 heads x 64 rows, d = 64, w = 512, fp32: 54 us; with every lane reading
+// its key's row from global memory 168 us).
 #include <cmath>
 
 #include "draft_internal.h"
@@ -55,184 +57,257 @@ template <> struct Vec<__nv_bfloat16> {
   }
 };
 
-template <typename T, int D>
-__device__ __forceinline__ float dot(const float* q, const T* k) {
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 16
-  for (int i = 0; i < D; i += Vec<T>::N) {
-    float x[Vec<T>::N];
-    Vec<T>::load(k + i, x);
-#pragma unroll
-    for (int j = 0; j < Vec<T>::N; ++j) s[j & 3] += q[i + j] * x[j];
-  }
-  return (s[0] + s[1]) + (s[2] + s[3]);
-}
-
 // phi(q) . phi(k), fq = phi(q)
-template <typename T, int D>
-__device__ __forceinline__ float phi_dot(const float* fq, const T* k, int phi) {
-  if (phi == RATTN_PHI_IDENTITY) return dot<T, D>(fq, k);
+template <int D>
+__device__ __forceinline__ float phi_dot(const float* fq, const float* k, int phi) {
   float m = -INFINITY, s = 0.f, n = 0.f;
   if (phi == RATTN_PHI_SOFTMAX)
-#pragma unroll 4
-    for (int i = 0; i < D; i += Vec<T>::N) {
-      float x[Vec<T>::N];
-      Vec<T>::load(k + i, x);
-#pragma unroll
-      for (int j = 0; j < Vec<T>::N; ++j) m = fmaxf(m, x[j]);
-    }
-#pragma unroll 4
-  for (int i = 0; i < D; i += Vec<T>::N) {
-    float x[Vec<T>::N];
-    Vec<T>::load(k + i, x);
-#pragma unroll
-    for (int j = 0; j < Vec<T>::N; ++j) {
-      const float e = phi == RATTN_PHI_SOFTMAX ? expf(x[j] - m) : fmaxf(x[j], 0.f);
-      s += fq[i + j] * e;
-      n += e;
-    }
+#pragma unroll 8
+    for (int i = 0; i < D; ++i) m = fmaxf(m, k[i]);
+#pragma unroll 8
+  for (int i = 0; i < D; ++i) {
+    const float e = phi == RATTN_PHI_SOFTMAX ? expf(k[i] - m) : phi == RATTN_PHI_RELU ? fmaxf(k[i], 0.f) : k[i];
+    s += fq[i] * e;
+    n += e;
   }
   return phi == RATTN_PHI_SOFTMAX ? s / n : s;
 }
 
-template <typename T, int D>
+template <int D, int RW> struct GenericPlan {             // floats of shared memory
+  static constexpr int KS = D + 4;                          // a key's row: lanes 16 bytes apart modulo 128
+  static constexpr int K = 0, V = K + 32 * KS, Q = V + 32 * D, F = Q + DG_WARPS * RW * D, END = F + DG_WARPS * RW * D;
+};
+
+// RW: rows per warp
+template <typename T, int D, int RW>
 __global__ void __launch_bounds__(DG_WARPS * 32) draft_generic_kernel(const __grid_constant__ DraftArgs a) {
-  constexpr int C = D / 32;
-  __shared__ __align__(16) float q_s[DG_WARPS][D];
-  __shared__ __align__(16) float f_s[DG_WARPS][D];
+  using P = GenericPlan<D, RW>;
+  constexpr int C = D / 32, ROWS = DG_WARPS * RW;
+  extern __shared__ __align__(16) float sm[];
   __shared__ int par[kMaxNodes], depth[kMaxNodes];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int R = a.group * a.N, blocks = (R + DG_WARPS - 1) / DG_WARPS;
-  const int z = blockIdx.x / blocks, b = z / a.H_kv, hk = z % a.H_kv;
-  const int row = (blockIdx.x % blocks) * DG_WARPS + warp, n = row / a.group, h = hk * a.group + row % a.group;
+  const int R = a.group * a.N, blocks = (R + ROWS - 1) / ROWS;
+  const int z = blockIdx.x / blocks, b = z / a.H_kv, hk = z % a.H_kv, row0 = (blockIdx.x % blocks) * ROWS + warp * RW;
+  float* k_s = sm + P::K;
+  float* v_s = sm + P::V;
+  float* q_s = sm + P::Q + warp * RW * D;
+  float* f_s = sm + P::F + warp * RW * D;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");        // the inputs may come from the kernel before
   for (int i = threadIdx.x; i < a.N; i += DG_WARPS * 32) par[i] = a.parents[(size_t)b * a.N + i];
   __syncthreads();
   for (int i = threadIdx.x; i < a.N; i += DG_WARPS * 32) depth[i] = node_depth(par, i);
   __syncthreads();
-  const int e = row < R ? depth[n] : -1;
-  if (e < 0) return;
-  NodeSet path;
-  node_path(par, n, &path);
   const int pos = entry_pos(a, b), w = a.w;
   const RingAge age(pos, w);
 
-  const T* qr = static_cast<const T*>(a.q) + node_at(a, b, h, a.H_q, n);
-  float x[C], fx[C];
+  int e[RW];                                                // depth of the row's node; -1: no node
+  NodeSet path[RW];
+  float m[RW], l[RW], o[RW][C], r[RW][C];
 #pragma unroll
-  for (int i = 0; i < C; ++i) q_s[warp][lane + 32 * i] = x[i] = (float)qr[lane + 32 * i];
-  if (a.phi == RATTN_PHI_SOFTMAX) {
-    float m = x[0], s = 0.f;
+  for (int k = 0; k < RW; ++k) {
+    const int row = row0 + k, n = min(row, R - 1) / a.group, h = hk * a.group + min(row, R - 1) % a.group;
+    e[k] = row < R ? depth[n] : -1;
 #pragma unroll
-    for (int i = 1; i < C; ++i) m = fmaxf(m, x[i]);
-    m = wmax(m);
+    for (int i = 0; i < kMaxNodes / 32; ++i) path[k].w[i] = 0u;
+    if (e[k] >= 0) node_path(par, n, &path[k]);
+    const T* qr = static_cast<const T*>(a.q) + node_at(a, b, h, a.H_q, n);
+    float x[C], fx[C];
 #pragma unroll
-    for (int i = 0; i < C; ++i) s += fx[i] = expf(x[i] - m);
-    s = wsum(s);
+    for (int i = 0; i < C; ++i) q_s[k * D + lane + 32 * i] = x[i] = (float)qr[lane + 32 * i];
+    if (a.phi == RATTN_PHI_SOFTMAX) {
+      float mx = x[0], s = 0.f;
 #pragma unroll
-    for (int i = 0; i < C; ++i) fx[i] /= s;
-  } else {
+      for (int i = 1; i < C; ++i) mx = fmaxf(mx, x[i]);
+      mx = wmax(mx);
 #pragma unroll
-    for (int i = 0; i < C; ++i) fx[i] = a.phi == RATTN_PHI_RELU ? fmaxf(x[i], 0.f) : x[i];
-  }
+      for (int i = 0; i < C; ++i) s += fx[i] = expf(x[i] - mx);
+      s = wsum(s);
 #pragma unroll
-  for (int i = 0; i < C; ++i) f_s[warp][lane + 32 * i] = fx[i];
-  __syncwarp();
-
-  float m = -INFINITY, l = 0.f, o[C], r[C];
+      for (int i = 0; i < C; ++i) fx[i] /= s;
+    } else {
 #pragma unroll
-  for (int i = 0; i < C; ++i) o[i] = r[i] = 0.f;
-  // keys base + lane * stride of up to 32: near / far say which of them the row sees how
-  auto block = [&](const T* kb, const T* vb, size_t stride, bool near, bool far) {
-    const uint32_t nears = __ballot_sync(0xffffffffu, near), fars = __ballot_sync(0xffffffffu, far);
-    if ((nears | fars) == 0u) return;
-    float p = near ? dot<T, D>(q_s[warp], kb + lane * stride) * a.scale : -INFINITY;
-    if (nears) {
-      const float m_new = fmaxf(m, wmax(p)), safe = m_new == -INFINITY ? 0.f : m_new, f = expf(m - safe);
-      l *= f;
-#pragma unroll
-      for (int i = 0; i < C; ++i) o[i] *= f;
-      m = m_new;
-      p = near ? expf(p - safe) : 0.f;
-      l += wsum(p);
+      for (int i = 0; i < C; ++i) fx[i] = a.phi == RATTN_PHI_RELU ? fmaxf(x[i], 0.f) : x[i];
     }
-    if (far) p = phi_dot<T, D>(f_s[warp], kb + lane * stride, a.phi);
-    if (nears == 0xffffffffu) {                              // all of them near: eight values on their way at a time
-      for (int j0 = 0; j0 < 32; j0 += 8) {
-        T vv[8][C];
+    m[k] = -INFINITY;
+    l[k] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+    for (int i = 0; i < C; ++i) {
+      f_s[k * D + lane + 32 * i] = fx[i];
+      o[k][i] = r[k][i] = 0.f;
+    }
+  }
+
+  // the keys base .. base + n - 1 (rows `stride` apart) to shared memory; then near / far say how the warp's rows see them
+  auto load = [&](const T* kb, const T* vb, size_t stride, int n) {
+    __syncthreads();                                        // everybody has read the tile before
+    constexpr int PER = D / Vec<T>::N;
+#pragma unroll 4
+    for (int c = threadIdx.x; c < 32 * PER; c += DG_WARPS * 32) {
+      const int j = c / PER, at = (c % PER) * Vec<T>::N;
+      if (j >= n) break;
+      float x[Vec<T>::N], y[Vec<T>::N];
+      Vec<T>::load(kb + j * stride + at, x);
+      Vec<T>::load(vb + j * stride + at, y);
 #pragma unroll
-          for (int i = 0; i < C; ++i) vv[j][i] = vb[(j0 + j) * stride + lane + 32 * i];
+      for (int i = 0; i < Vec<T>::N; i += 4) {
+        *reinterpret_cast<float4*>(k_s + j * P::KS + at + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        *reinterpret_cast<float4*>(v_s + j * D + at + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+      }
+    }
+    __syncthreads();
+  };
+  auto tile = [&](const bool (&near)[RW], const bool (&far)[RW]) {
+    float p[RW];
+    uint32_t nears[RW], fars[RW], all = 0xffffffffu, any = 0u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float pj = __shfl_sync(0xffffffffu, p, j0 + j);
+    for (int k = 0; k < RW; ++k) {
+      nears[k] = __ballot_sync(0xffffffffu, near[k]);
+      fars[k] = __ballot_sync(0xffffffffu, far[k]);
+      all &= nears[k];
+      any |= nears[k] | fars[k];
+      p[k] = 0.f;
+    }
+    if (any == 0u) return;
+    if (any >> lane & 1u) {                                  // (rows of the tile behind its last key hold another tile's)
+#pragma unroll 4
+      for (int i = 0; i < D; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(k_s + lane * P::KS + i);
 #pragma unroll
-          for (int i = 0; i < C; ++i) o[i] += pj * (float)vv[j][i];
+        for (int k = 0; k < RW; ++k) {
+          const float4 q = *reinterpret_cast<const float4*>(q_s + k * D + i);
+          p[k] += (q.x * x.x + q.y * x.y) + (q.z * x.z + q.w * x.w);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < RW; ++k) {
+      p[k] = near[k] ? p[k] * a.scale : -INFINITY;
+      if (nears[k]) {
+        const float m_new = fmaxf(m[k], wmax(p[k])), safe = m_new == -INFINITY ? 0.f : m_new, f = expf(m[k] - safe);
+        l[k] *= f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) o[k][i] *= f;
+        m[k] = m_new;
+        p[k] = near[k] ? expf(p[k] - safe) : 0.f;
+        l[k] += wsum(p[k]);
+      }
+      if (far[k]) p[k] = phi_dot<D>(f_s + k * D, k_s + lane * P::KS, a.phi);
+    }
+    if (all == 0xffffffffu) {
+#pragma unroll 4
+      for (int j = 0; j < 32; ++j) {
+        float v[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = v_s[j * D + lane + 32 * i];
+#pragma unroll
+        for (int k = 0; k < RW; ++k) {
+          const float pj = __shfl_sync(0xffffffffu, p[k], j);
+#pragma unroll
+          for (int i = 0; i < C; ++i) o[k][i] += pj * v[i];
         }
       }
       return;
     }
-    for (uint32_t todo = nears | fars; todo; todo &= todo - 1) {
+    for (uint32_t todo = any; todo; todo &= todo - 1) {
       const int j = __ffs(todo) - 1;
-      const float pj = __shfl_sync(0xffffffffu, p, j);
-      const T* vr = vb + j * stride;
-      const bool is_near = (nears >> j) & 1u;
+      float v[C];
 #pragma unroll
-      for (int i = 0; i < C; ++i) {
-        const float vv = (float)vr[lane + 32 * i];
-        if (is_near) o[i] += pj * vv;
-        else r[i] += pj * vv;
+      for (int i = 0; i < C; ++i) v[i] = v_s[j * D + lane + 32 * i];
+#pragma unroll
+      for (int k = 0; k < RW; ++k) {
+        const float pj = __shfl_sync(0xffffffffu, p[k], j);
+        if (nears[k] >> j & 1u)
+#pragma unroll
+          for (int i = 0; i < C; ++i) o[k][i] += pj * v[i];
+        else if (fars[k] >> j & 1u)
+#pragma unroll
+          for (int i = 0; i < C; ++i) r[k][i] += pj * v[i];
       }
     }
   };
   const T* kr = static_cast<const T*>(a.k_ring) + (size_t)z * w * D;
   const T* vr = static_cast<const T*>(a.v_ring) + (size_t)z * w * D;
   const int held = min(pos, w);                             // slots 0 .. held-1 hold tokens
+  bool near[RW], far[RW];
   for (int s0 = 0; s0 < held; s0 += 32) {
+    load(kr + (size_t)s0 * D, vr + (size_t)s0 * D, D, min(32, held - s0));
     const int rank = s0 + lane < held ? age.rank(s0 + lane) : -1;
-    block(kr + (size_t)s0 * D, vr + (size_t)s0 * D, D, rank >= age.first && rank >= e, rank >= age.first && rank < e);
+#pragma unroll
+    for (int k = 0; k < RW; ++k) {
+      near[k] = e[k] >= 0 && rank >= age.first && rank >= e[k];
+      far[k] = rank >= age.first && rank < e[k];
+    }
+    tile(near, far);
   }
   const size_t step = a.layout == RATTN_LAYOUT_BHTD ? (size_t)D : (size_t)a.H_kv * D;
   for (int j0 = 0; j0 < a.N; j0 += 32) {
     const size_t at = node_at(a, b, hk, a.H_kv, j0);
-    const bool mine = (path.w[j0 >> 5] >> lane) & 1u, near = mine && e - depth[j0 + lane] <= w;
-    block(static_cast<const T*>(a.k) + at, static_cast<const T*>(a.v) + at, step, near, mine && !near);
+    load(static_cast<const T*>(a.k) + at, static_cast<const T*>(a.v) + at, step, min(32, a.N - j0));
+#pragma unroll
+    for (int k = 0; k < RW; ++k) {
+      const bool mine = (path[k].w[j0 >> 5] >> lane) & 1u;
+      near[k] = mine && e[k] - depth[j0 + lane] <= w;
+      far[k] = mine && !near[k];
+    }
+    tile(near, far);
   }
   const float* S = a.state + (size_t)z * D * D;
-#pragma unroll 16
+#pragma unroll 8
   for (int f = 0; f < D; ++f) {
-    const float fq = f_s[warp][f];
+    float x[C];
 #pragma unroll
-    for (int i = 0; i < C; ++i) r[i] += fq * S[f * D + lane + 32 * i];
+    for (int i = 0; i < C; ++i) x[i] = S[f * D + lane + 32 * i];
+#pragma unroll
+    for (int k = 0; k < RW; ++k) {
+      const float fq = f_s[k * D + f];
+#pragma unroll
+      for (int i = 0; i < C; ++i) r[k][i] += fq * x[i];
+    }
   }
-  float so = 0.f, sr = 0.f;
 #pragma unroll
-  for (int i = 0; i < C; ++i) {
-    o[i] /= l;
-    so += o[i] * o[i];
-    sr += r[i] * r[i];
-  }
-  const float is = rsqrtf(wsum(so) / D + a.eps), ir = rsqrtf(wsum(sr) / D + a.eps);
-  T* out = static_cast<T*>(a.out) + node_at(a, b, h, a.H_q, n);
+  for (int k = 0; k < RW; ++k) {
+    if (e[k] < 0) continue;                                  // (the same for the warp)
+    const int n = (row0 + k) / a.group, h = hk * a.group + (row0 + k) % a.group;
+    float so = 0.f, sr = 0.f;
 #pragma unroll
-  for (int i = 0; i < C; ++i) {
-    const int c = lane + 32 * i;
-    const float gs = a.gamma_swa ? a.gamma_swa[(size_t)h * D + c] : 1.f, gr = a.gamma_rla ? a.gamma_rla[(size_t)h * D + c] : 1.f;
-    out[c] = (T)(gs * o[i] * is + gr * r[i] * ir);
+    for (int i = 0; i < C; ++i) {
+      o[k][i] /= l[k];
+      so += o[k][i] * o[k][i];
+      sr += r[k][i] * r[k][i];
+    }
+    const float is = rsqrtf(wsum(so) / D + a.eps), ir = rsqrtf(wsum(sr) / D + a.eps);
+    T* out = static_cast<T*>(a.out) + node_at(a, b, h, a.H_q, n);
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = lane + 32 * i;
+      const float gs = a.gamma_swa ? a.gamma_swa[(size_t)h * D + c] : 1.f, gr = a.gamma_rla ? a.gamma_rla[(size_t)h * D + c] : 1.f;
+      out[c] = (T)(gs * o[k][i] * is + gr * r[k][i] * ir);
+    }
   }
 }
 
-template <typename T, int D>
-cudaError_t launch_generic_as(const DraftArgs& a, cudaStream_t s) {
-  const int blocks = (a.group * a.N + DG_WARPS - 1) / DG_WARPS;
+template <typename T, int D, int RW>
+cudaError_t launch_generic_rows(const DraftArgs& a, cudaStream_t s) {
+  constexpr int smem = GenericPlan<D, RW>::END * (int)sizeof(float), rows = DG_WARPS * RW;
+  cudaError_t e = allow_smem<draft_generic_kernel<T, D, RW>>(smem);
+  if (e != cudaSuccess) return e;
+  const int blocks = (a.group * a.N + rows - 1) / rows;
   KernelTimer kt("draft_attention", s);
-  const cudaError_t e = launch_pdl(draft_generic_kernel<T, D>, dim3((unsigned)((long long)a.B * a.H_kv * blocks)),
-                                   dim3(DG_WARPS * 32), 0, s, true, a);
+  e = launch_pdl(draft_generic_kernel<T, D, RW>, dim3((unsigned)((long long)a.B * a.H_kv * blocks)), dim3(DG_WARPS * 32), smem, s, true, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   return cudaGetLastError();
+}
+
+// Four rows to a warp share its reads of keys and values; where that leaves SMs without a CTA, one.
+template <typename T, int D>
+cudaError_t launch_generic_as(const DraftArgs& a, cudaStream_t s) {
+  int n_sm = 0;
+  const cudaError_t e = sm_count(&n_sm);
+  if (e != cudaSuccess) return e;
+  const long long ctas = (long long)a.B * a.H_kv * ((a.group * a.N + 4 * DG_WARPS - 1) / (4 * DG_WARPS));
+  return ctas >= n_sm ? launch_generic_rows<T, D, 4>(a, s) : launch_generic_rows<T, D, 1>(a, s);
 }
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
