@@ -607,11 +607,9 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 #ifdef RATTN_DEBUG_KNOBS
     if (a.debug_wait == 2 && rank == CS - 1) bars->abort = 1;     // as if one of its waits had run out
 #endif
-  } else if (warp == 5) {
-    window_load(maps, it, smem, bars);
-    if (!CL) load_s(0, 0);
   } else {
-    if (warp == 6) window_clean(d, it, smem, bars, lane);
+    if (warp == 5) window_load(maps, it, smem, bars);
+    else if (warp == 6) window_clean(d, it, smem, bars, lane);
     else window_scores(it, smem, bars, tS);
     // nodes that some row has more than w levels up; the far keys, as soon as there is room for them
     if (dmax > d.w && tid == 192) {
@@ -620,10 +618,11 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         if (bars->depth[j] >= 0 && bars->depth[j] < dmax - d.w) bars->far_node[n++] = (short)j;
       bars->n_far_node = n;
     }
-    named_sync(1, 64);
+    __syncwarp();
+    named_sync(1, 96);
     mbar_wait(&bars->scored, 0u, &bars->abort);
     __syncwarp();
-    if (rank == 0) build_k(0, corner + bars->n_far_node, 6, 2);
+    if (rank == 0) build_k(0, corner + bars->n_far_node, 5, 3);
     if (!CL) load_s(0, 0);
   }
   __syncthreads();                       // the window's products are complete, its slots free, all nodes looked at
