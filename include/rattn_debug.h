@@ -10,7 +10,8 @@
  * anything, and its waits give up after 2^15 polls instead of 2^21:
  *   1  the tensor-core forward's first row group leaves out ONE mbarrier arrival (a plain
  *      arrive with no asynchronous copy behind it) in the first work unit of every CTA, so
- *      that a wait does run out;
+ *      that a wait does run out; so does the last CTA of each cluster, or every single CTA, of the
+ *      draft attention's tensor-core kernel;
  *   2  in every tensor-core kernel whose threads share named barriers, some of these threads
  *      treat their first wait as run out while the others have passed the same wait.
  *   3  rattn_forward_status finds that the scratch pool cannot be given back;

@@ -68,7 +68,7 @@ struct TcArgs {
   DraftArgs d;
   int row_tiles, rows_per_tile, cluster;
   float scale_log2, inv_group;
-  int debug_wait;                        // debug build only, 2: a wait counts as run out
+  int debug_wait;                        // debug build only, 1: an arrival is left out, 2: a wait counts as run out
 };
 struct alignas(64) TcMaps {
   CUtensorMap k_ring, v_ring;            // [B*H_kv, w, 128], box 64 columns x 64 slots
@@ -194,13 +194,15 @@ __device__ __forceinline__ void mma_weights(uint32_t o, uint32_t p, uint32_t v, 
 
 // Scores and products are issued by two warps: with its waits (some 300 cycles each, satisfied or not), its issue slots (65 per
 // instruction) and its commits one warp took 2.1 - 2.4k cycles a tile, the row warps take 1.5k.
+// A role whose wait has run out issues nothing more: what it would overwrite or read may still be on its way.
 __device__ void window_scores(const Item& it, unsigned char* smem, Bars* bars, uint32_t tS) {
   const uint32_t sQ = smem_u32(smem), sR = sQ + DA_OFF_RING;
-  mbar_wait_warp(&bars->q_full, 0u, &bars->abort);
-  for (int t = 0; t < it.nt; ++t) {
+  bool ok = mbar_wait_warp(&bars->q_full, 0u, &bars->abort);
+  for (int t = 0; t < it.nt && ok; ++t) {
     const int i = use_k(t), slot = i % DA_NS;
-    mbar_wait_warp(&bars->full[slot], (uint32_t)(i / DA_NS) & 1u, &bars->abort);
-    if (t >= 2) mbar_wait_warp(&bars->pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, &bars->abort);     // its weights lay there
+    ok = mbar_wait_warp(&bars->full[slot], (uint32_t)(i / DA_NS) & 1u, &bars->abort);
+    if (ok && t >= 2) ok = mbar_wait_warp(&bars->pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, &bars->abort);     // its weights lay there
+    if (!ok) break;
     tc_fence_after();
     mma_scores(tS + 64 * (t & 1), sQ, sR + slot * HT_BYTES);
     mma_commit(&bars->s_full[t & 1]);
@@ -212,9 +214,10 @@ __device__ void window_products(const Item& it, unsigned char* smem, Bars* bars,
   const uint32_t sR = smem_u32(smem) + DA_OFF_RING;
   for (int t = 0; t < it.nt; ++t) {
     const int i = use_v(t, it.nt), slot = i % DA_NS;
-    if (needs_cleaning(it, it.t0 + t)) mbar_wait_warp(&bars->clean[it.t0 + t - first_unclean(it)], 0u, &bars->abort);
-    else mbar_wait_warp(&bars->full[slot], (uint32_t)(i / DA_NS) & 1u, &bars->abort);
-    mbar_wait_warp(&bars->p_ready[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
+    bool ok = needs_cleaning(it, it.t0 + t) ? mbar_wait_warp(&bars->clean[it.t0 + t - first_unclean(it)], 0u, &bars->abort)
+                                            : mbar_wait_warp(&bars->full[slot], (uint32_t)(i / DA_NS) & 1u, &bars->abort);
+    if (ok) ok = mbar_wait_warp(&bars->p_ready[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
+    if (!ok) break;
     tc_fence_after();
     mma_weights(tO, tS + 64 * (t & 1), sR + slot * HT_BYTES, t > 0, 4);
     mma_commit(&bars->pv_done[t & 1]);
@@ -222,17 +225,20 @@ __device__ void window_products(const Item& it, unsigned char* smem, Bars* bars,
   }
 }
 
-__device__ void window_load(const TcMaps& m, const Item& it, unsigned char* smem, Bars* bars) {
+// Returns how many uses have been asked for: all, unless a wait has run out (a slot whose last load may still be on its way is
+// not armed again).
+__device__ int window_load(const TcMaps& m, const Item& it, unsigned char* smem, Bars* bars) {
   for (int i = DA_NS; i < 2 * it.nt; ++i) {
-    mbar_wait_warp(&bars->free_[i % DA_NS], (uint32_t)(i / DA_NS - 1) & 1u, &bars->abort);
+    if (!mbar_wait_warp(&bars->free_[i % DA_NS], (uint32_t)(i / DA_NS - 1) & 1u, &bars->abort)) return i;
     load_use(m, it, smem, bars, i);
   }
+  return 2 * it.nt;
 }
 
 __device__ void window_clean(const DraftArgs& d, const Item& it, unsigned char* smem, Bars* bars, int cid) {
   for (int T = first_unclean(it); T < it.t0 + it.nt; ++T) {
     const int n = T - first_unclean(it), slot = use_v(T - it.t0, it.nt) % DA_NS;
-    mbar_wait(&bars->landed[n], 0u, &bars->abort);
+    if (!mbar_wait_warp(&bars->landed[n], 0u, &bars->abort)) return;
     unsigned char* tile = smem + DA_OFF_RING + slot * HT_BYTES;
     if (T < it.n_ring) {
       for (int c = cid + (it.held & 63) * 16; c < 64 * 16; c += 32) *reinterpret_cast<uint4*>(tile + at_half(c >> 4, c & 15)) = make_uint4(0u, 0u, 0u, 0u);
@@ -352,6 +358,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   const int e = node >= 0 ? bars->depth[node] : -1;
   const uint32_t lanes = (uint32_t)((tid & 96) << 16);       // TMEM lane of the row
   uint64_t near0 = 0, near1 = 0, far0 = 0, far1 = 0;         // nodes 0 - 63, 64 - 127 of its path, up to w levels up and further
+  int uses = 0;                                              // of the ring's slots, asked for (loader warp)
   float m_ref = -INFINITY, l = 0.f;
   float inv_phi = 1.f;                                       // of the row's feature map
   // the slots behind the window's last use, oldest first: 0 - 2 are free once the last scores have been formed
@@ -536,7 +543,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
           keep = T > it.n_ring ? near1 : near0;
           all = false;
         }
-        mbar_wait(&bars->s_full[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
+        if (!mbar_wait_warp(&bars->s_full[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort)) break;
         tc_fence_after();
         float x[64];
         tmem_ld32(ts, reinterpret_cast<float(&)[32]>(x[0]));
@@ -556,9 +563,8 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
           const float m_new = fmaxf(m_ref, mx);
           if (t > 0) {
             const float f = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
-            mbar_wait(&bars->pv_done[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1u, &bars->abort);
+            if (!mbar_wait_warp(&bars->pv_done[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1u, &bars->abort)) break;
             tc_fence_after();
-            __syncwarp();
 #pragma unroll 1
             for (int c = 0; c < 8; ++c) {
               float o[16];
@@ -593,6 +599,9 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
         l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
         tmem_wait_st();
         tc_fence_before();
+#ifdef RATTN_DEBUG_KNOBS
+        if (!(a.debug_wait == 1 && t == 0 && tid == 0 && rank == CS - 1))             // an arrival that never comes
+#endif
         mbar_arrive(&bars->p_ready[t & 1]);
       }
     }
@@ -608,7 +617,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     if (a.debug_wait == 2 && rank == CS - 1) bars->abort = 1;     // as if one of its waits had run out
 #endif
   } else {
-    if (warp == 5) window_load(maps, it, smem, bars);
+    if (warp == 5) uses = window_load(maps, it, smem, bars);
     else if (warp == 6) window_clean(d, it, smem, bars, lane);
     else window_scores(it, smem, bars, tS);
     // nodes that some row has more than w levels up; the far keys, as soon as there is room for them
@@ -625,9 +634,12 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     if (rank == 0) build_k(0, corner + bars->n_far_node, 5, 3);
     if (!CL) load_s(0, 0);
   }
-  __syncthreads();                       // the window's products are complete, its slots free, all nodes looked at
+  // The window's products are complete, its slots free, all nodes looked at -- or a wait has run out, and all threads go to the
+  // end.
+  const bool gave_up = __syncthreads_or(*(volatile int*)&bars->abort) != 0;
   tc_fence_after();
 
+  if (!gave_up) {
   // ---- linear branch -----------------------------------------------------------------------------------------------
   unsigned char* slots = smem + DA_OFF_RING;
   float* stat = reinterpret_cast<float*>(smem + DA_OFF_STAT);
@@ -931,6 +943,10 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
    }
   }
+  } else if (CL) {                                           // (the others learn of it behind this barrier)
+    cluster_arrive();
+    cluster_wait();
+  }
   if (*(volatile int*)&bars->abort) {
     // a wait ran out: what is still in flight gets a bounded time to land before the memory goes away
     if (warp == 7) mma_commit(&bars->drain);
@@ -939,11 +955,10 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       for (int i = 0; i < kWaitPolls && !mbar_try_wait(&bars->drain, 0u); ++i) {}
     }
     if (warp == 5) {
-      const int uses = 2 * it.nt;
       for (int i = max(0, uses - DA_NS); i < uses; ++i)
         for (int p = 0; p < kWaitPolls && !mbar_try_wait(&bars->full[i % DA_NS], (uint32_t)(i / DA_NS) & 1u); ++p) {}
-      for (int i = 0; i < it.t0 + it.nt - first_unclean(it); ++i)
-        for (int p = 0; p < kWaitPolls && !mbar_try_wait(&bars->landed[i], 0u); ++p) {}
+      for (int T = first_unclean(it); T < it.t0 + it.nt && use_v(T - it.t0, it.nt) < uses; ++T)
+        for (int p = 0; p < kWaitPolls && !mbar_try_wait(&bars->landed[T - first_unclean(it)], 0u); ++p) {}
     }
     if (tid == 0) g_draft_status = RATTN_ERR_TIMEOUT;
   }

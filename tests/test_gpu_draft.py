@@ -517,10 +517,12 @@ def test_attention_of_a_batch(B, Hq, Hkv, N, w, top, kind, layout):
         check(out[0][i][heads], ref, "bf16", i)
 
 
-@pytest.mark.parametrize("B,Hkv,pos", [(1, 2, 900), (40, 8, 300)])
-def test_a_wait_that_runs_out_is_reported(B, Hkv, pos):
-    """The debug build takes a wait of the attention kernel as run out: the call ends, says so once, writes no row, and the next
-    call on the same buffers is right (clusters of CTAs, of which one gives up, and single ones)."""
+@pytest.mark.parametrize("how", [1, 2])
+@pytest.mark.parametrize("B,Hkv,w,pos", [(1, 2, 256, 900), (40, 8, 256, 300), (9, 8, 1024, 2000), (20, 8, 1024, 2000)])
+def test_a_wait_that_runs_out_is_reported(B, Hkv, w, pos, how):
+    """In the debug build one arrival of the attention kernel never comes, or a wait counts as run out: the call ends, says so once,
+    writes no row, and the next call on the same buffers is right (clusters of CTAs, of which one gives up, and single ones; more
+    loads than slots, so that some are still to be asked for)."""
     import ctypes
 
     from paper_2506_15545_b200 import build
@@ -530,7 +532,7 @@ def test_a_wait_that_runs_out_is_reported(B, Hkv, pos):
     L.rattn_draft_status.argtypes = [vp]
     g = torch.Generator(device="cuda").manual_seed(2)
     rnd = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()  # noqa: E731
-    N, w, d = 6, 256, 128
+    N, d = 6, 128
     q, k, v, kr, vr = rnd(B, Hkv, N, d), rnd(B, Hkv, N, d), rnd(B, Hkv, N, d), rnd(B, Hkv, w, d), rnd(B, Hkv, w, d)
     state, out = torch.randn(B, Hkv, d, d, device="cuda", generator=g), torch.full_like(q, 7.0)
     par = torch.tensor([[-1, 0, 1, 1, 2, 0]] * B, dtype=torch.int32, device="cuda")
@@ -540,7 +542,7 @@ def test_a_wait_that_runs_out_is_reported(B, Hkv, pos):
     p.B, p.H_q, p.H_kv, p.N, p.d, p.w, p.dtype, p.scale, p.eps, p.pos = B, Hkv, Hkv, N, d, w, R.RATTN_BF16, 0.1, 1e-6, pos
     stream = vp(torch.cuda.current_stream().cuda_stream)
     try:
-        L.rattn_debug_withhold_arrival(2)
+        L.rattn_debug_withhold_arrival(how)
         assert L.rattn_draft_attention(ctypes.byref(p), stream) == 0
         assert L.rattn_draft_status(stream) == -7
         assert (out == 7.0).all()
