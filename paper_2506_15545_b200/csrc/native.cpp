@@ -84,6 +84,15 @@ struct Args {
   }
   // what ctypes did with an integer field or argument: the low 32 bits
   int32_t i32() { return static_cast<int32_t>(integer()); }
+  // an integer that a call with checks of its own refuses to shorten
+  int32_t exact_i32(const char* what) {
+    const long v = integer();
+    if (v != static_cast<int32_t>(v)) {
+      PyErr_Format(PyExc_ValueError, "%s does not fit 32 bits", what);
+      throw Raised{};
+    }
+    return static_cast<int32_t>(v);
+  }
   float real() {
     const double v = PyFloat_AsDouble(next());
     if (v == -1.0 && PyErr_Occurred()) throw Raised{};
@@ -444,7 +453,7 @@ PyObject* draft_attention(Args a) {
   x.k = a.tensor(); x.v = a.tensor();
   const at::Tensor parents = a.tensor();
   x.k_ring = a.tensor(); x.v_ring = a.tensor(); x.state = a.tensor();
-  x.p.pos = a.i32();
+  x.p.pos = a.exact_i32("pos");
   x.p.scale = a.real();
   x.p.eps = a.real();
   const at::Tensor gs = a.maybe(), gr = a.maybe(), given = a.maybe();
@@ -475,7 +484,7 @@ PyObject* draft_commit(Args a) {
   x.k = a.tensor(); x.v = a.tensor();
   const at::Tensor path = a.tensor(), n = a.tensor();
   x.k_ring = a.tensor(); x.v_ring = a.tensor(); x.state = a.tensor();
-  x.p.pos = a.i32();
+  x.p.pos = a.exact_i32("pos");
   x.p.feature_map = a.i32();
   x.pos = a.maybe();
   x.p.layout = a.i32();

@@ -517,6 +517,65 @@ def test_attention_of_a_batch(B, Hq, Hkv, N, w, top, kind, layout):
         check(out[0][i][heads], ref, "bf16", i)
 
 
+@pytest.mark.parametrize("Hq,Hkv,B", [(4, 2, 2), (8, 8, 40)])
+@pytest.mark.parametrize("flags", [0, R.FLAG_FORCE_GENERIC])
+def test_the_largest_positions(Hq, Hkv, B, flags):
+    """A position matters by its remainder modulo w once the ring is full: the largest that are taken give the bits of a small one."""
+    N, w = 20, 100
+    s = Setup(B, Hq, Hkv, N, 128, w, "bf16", 2 * w + 47, "chain", seed=21)
+    small = s.run(flags=flags)
+    top = 2 ** 31 - 1 - w - R.DRAFT_MAX_NODES
+    top -= (top - 47) % w
+    s.pos = [top] * B
+    assert torch.equal(small, s.run(flags=flags)) and torch.equal(small, s.run(flags=flags, per_entry=False))
+    path = torch.arange(N, dtype=torch.int32, device="cuda").repeat(B, 1)
+    n = torch.full((B,), N, dtype=torch.int32, device="cuda")
+    caches = []
+    for pos in (2 * w + 47, top):
+        caches.append([s.k_ring.clone(), s.v_ring.clone(), s.state.clone()])
+        R.rattn_draft_commit(s.k.cuda(), s.v.cuda(), path, n, *caches[-1], pos)
+    assert all(torch.equal(a, b) for a, b in zip(*caches))
+    with pytest.raises(ValueError):
+        s.pos = [2 ** 32 + 47] * B
+        s.run(flags=flags, per_entry=False)
+    with pytest.raises(ValueError):
+        R.rattn_draft_commit(s.k.cuda(), s.v.cuda(), path, n, *caches[0], 2 ** 32)
+
+
+def test_two_calls_at_once():
+    """Calls on two streams share nothing but what they read: the same bits as one after the other, all operators at work."""
+    setups = [Setup(1, 8, 2, 6, 128, 512, "bf16", 700, "chain", seed=1), Setup(24, 8, 8, 30, 128, 192, "bf16", 300, "tree", seed=2)]
+    jobs = []
+    for s in setups:
+        B, N = s.parents.shape
+        p, q, u, g = _rows(B, N, 5003, B, "bf16", 2.0)
+        jobs.append(dict(q=s.q.cuda(), k=s.k.cuda(), v=s.v.cuda(), par=torch.tensor(s.parents, dtype=torch.int32, device="cuda"),
+                         p=p.cuda(), dq=q.cuda(), u=u.cuda(), tok=torch.randint(0, 5003, (B, N), generator=g, dtype=torch.int32).cuda(),
+                         cache=[s.k_ring, s.v_ring, s.state], pos=s.pos[0], scale=s.scale))
+
+    def step(j):
+        path, n, token = R.rattn_draft_verify(j["tok"], j["par"], j["p"], j["dq"], j["u"])
+        cache = [x.clone() for x in j["cache"]]
+        y = R.rattn_draft_attention(j["q"], j["k"], j["v"], j["par"], *cache, j["pos"], scale=j["scale"])
+        R.rattn_draft_commit(j["k"], j["v"], path, n, *cache, j["pos"])
+        rows = torch.tensor([[D.path_of(par, i) is not None for i in range(len(par))] for par in j["par"].tolist()])
+        return [path, n, token, y.transpose(1, 2)[rows.cuda()]] + cache
+
+    want = [step(j) for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[], []]
+    for _ in range(10):
+        for i, j in enumerate(jobs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(step(j))
+    torch.cuda.synchronize()
+    assert R.rattn_draft_status() == 0
+    for w_, runs in zip(want, got):
+        for r in runs:
+            assert all(torch.equal(a, b) for a, b in zip(w_, r))
+
+
 @pytest.mark.parametrize("how", [1, 2])
 @pytest.mark.parametrize("B,Hkv,w,pos", [(1, 2, 256, 900), (40, 8, 256, 300), (9, 8, 1024, 2000), (20, 8, 1024, 2000)])
 def test_a_wait_that_runs_out_is_reported(B, Hkv, w, pos, how):
