@@ -16,8 +16,8 @@
 // Linear branch, O_rla = phi(Q) S + (phi(Q) phi(K_far)^T masked) V_far: phi(Q) replaces Q without its normalisation (which the
 // rows apply at the end) as a bf16 pair, S is split likewise, and three products give 16 bits of both; K_far are the at
 // most 127 tokens that have left some row's window (slots of rank < depth; nodes more than w levels up), gathered into a tile.
-// The window output waits in TMEM meanwhile, normalised: its values are then at most sqrt(128), and 16 bits of fixed point
-// hold them to 1.7e-4 (fp16 would be off by 2^-11 of the larger ones, a quarter of the output's own rounding).  y leaves through
+// The window output waits in TMEM meanwhile, where the far keys' scores and weights leave it 96 of its 128 columns: each value is
+// rounded to the upper 24 bits of its fp32 form, off by 2^-17 of itself whatever the row's size, eps or gain.  y leaves through
 // shared memory, a warp per row, where gains are read once per row and coalesced.
 //
 // Few heads (B H_kv row tiles below the SMs): a cluster of CTAs shares the tiles of keys and the features of S; the partial
@@ -44,7 +44,6 @@ constexpr int DA_OFF_OX = DA_SMEM;                           // cluster: [rows][
 constexpr int DA_OFF_STAT = DA_OFF_OX + 2 * DA_CLUSTER_ROWS * 512;
 constexpr int DA_SMEM_CLUSTER = DA_OFF_STAT + 2 * DA_CLUSTER_ROWS * 4;
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float PARK = 32767.f / 11.32f;                     // steps per unit of a normalised row of 128 (at most 11.314)
 
 __device__ int g_draft_status;           // RATTN_ERR_TIMEOUT once a bounded wait has expired
 
@@ -56,11 +55,15 @@ struct Bars {
   uint32_t tmem_base;
   int abort;
   uint32_t bad[kMaxNodes / 32];          // nodes with a value that is not finite
-  signed char par[kMaxNodes];            // -2: no node
   signed char depth[kMaxNodes];          // -1: no node
-  short far_node[kMaxNodes];             // nodes that some row has more than w levels up
   int n_far_node, deepest;
-  unsigned char odd[TILE];               // rows whose window output is not finite
+  union {
+    struct {
+      signed char par[kMaxNodes];        // -2: no node
+      short far_node[kMaxNodes];         // nodes that some row has more than w levels up
+    };
+    float window_scale[TILE];            // the output: what a row of the window branch is to be multiplied by
+  };
 };
 static_assert(sizeof(Bars) <= DA_SMEM - DA_OFF_BARS, "control block");
 
@@ -112,6 +115,21 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t a) {
   return v;
 }
 
+// Four floats in three words, each with the upper 24 of its bits (rounded: off by 2^-17 of the value at most): three in a word's upper
+// bytes, and the fourth's bytes in the lower ones.  (A NaN may come back as a number; its row's scale is NaN, too.)
+__device__ __forceinline__ void pack24(const float* x, uint32_t* w0, uint32_t* w1, uint32_t* w2) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(x[i]) + 0x80u;
+  *w0 = __byte_perm(u[0], u[3], 0x3217);
+  *w1 = __byte_perm(u[1], u[3], 0x3216);
+  *w2 = __byte_perm(u[2], u[3], 0x3215);
+}
+__device__ __forceinline__ float4 unpack24(uint32_t w0, uint32_t w1, uint32_t w2) {
+  const uint32_t last = __byte_perm(__byte_perm(w0, w1, 0x0400), w2, 0x3244);
+  return make_float4(__uint_as_float(w0 & 0xffffff00u), __uint_as_float(w1 & 0xffffff00u), __uint_as_float(w2 & 0xffffff00u),
+                     __uint_as_float(last & 0xffffff00u));
+}
 // Two floats as a word of leading parts (the upper halves of their bits, a byte permutation instead of a conversion) and one
 // of remainders, which a conversion rounds: off by 2^-16 of the value at most.
 __device__ __forceinline__ void split2(float a, float b, uint32_t* hi, uint32_t* lo) {
@@ -179,15 +197,15 @@ __device__ __forceinline__ void load_use(const TcMaps& m, const Item& it, unsign
 
 // S = Q K^T of one tile of 64 keys, D[128 x 64]
 __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k) { mma_k_kh(d, q, k); }
-// O += (hi + lo) V: A from TMEM, hi in columns 0-31, lo in 32-63
-__device__ __forceinline__ void mma_weights(uint32_t o, uint32_t p, uint32_t v, bool acc, int steps) {
+// O += (hi + lo) V: A from TMEM, hi in columns from 0 on, lo from `lo` on
+__device__ __forceinline__ void mma_weights(uint32_t o, uint32_t p, int lo, uint32_t v, bool acc, int steps) {
   constexpr uint32_t idesc = instr_desc(128, 128, 0, 1);
   const uint64_t v0 = mnmajor_base_h(v);
 #pragma unroll
   for (int part = 0; part < 2; ++part)
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (k < steps) mma_bf16_ts(o, p + 32 * part + 8 * k, v0 + kstep_mn(k), idesc, (acc || part > 0 || k > 0) ? 1u : 0u);
+      if (k < steps) mma_bf16_ts(o, p + lo * part + 8 * k, v0 + kstep_mn(k), idesc, (acc || part > 0 || k > 0) ? 1u : 0u);
 }
 
 // ---------------------------------------------------------------------------------------------- window loop, by role
@@ -219,7 +237,7 @@ __device__ void window_products(const Item& it, unsigned char* smem, Bars* bars,
     if (ok) ok = mbar_wait_warp(&bars->p_ready[t & 1], (uint32_t)(t >> 1) & 1u, &bars->abort);
     if (!ok) break;
     tc_fence_after();
-    mma_weights(tO, tS + 64 * (t & 1), sR + slot * HT_BYTES, t > 0, 4);
+    mma_weights(tO, tS + 64 * (t & 1), 32, sR + slot * HT_BYTES, t > 0, 4);
     mma_commit(&bars->pv_done[t & 1]);
     mma_commit(t + 1 < it.nt ? &bars->free_[slot] : &bars->o_full);      // (nothing follows into the last one's slot)
   }
@@ -309,7 +327,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   tc_fence_after();
   // (behind the allocation of TMEM: a kernel that is set up under this one may want some, too)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const uint32_t tmem = bars->tmem_base, tS = tmem, tO = tmem + 128;
+  const uint32_t tmem = bars->tmem_base, tS = tmem, tO = tmem + 128, tFar = tO + 96;     // tFar: scores, then weights of far keys
   asm volatile("griddepcontrol.wait;" ::: "memory");        // the inputs may come from the kernel before
   const Item it = make_item(a, rank);
 
@@ -672,13 +690,13 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       if ((j < 64 ? far0 : far1) >> (j & 63) & 1u) keep |= 1u << i;
     }
     float z[32];
-    tmem_ld32(tO + 64 + lanes, z);
+    tmem_ld32(tFar + lanes, z);
     tmem_wait_ld();
     uint32_t hi[16], lo[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) split2(keep >> (2 * i) & 1u ? z[2 * i] : 0.f, keep >> (2 * i + 1) & 1u ? z[2 * i + 1] : 0.f, &hi[i], &lo[i]);
-    tmem_st16(tO + 64 + lanes, hi);
-    tmem_st16(tO + 96 + lanes, lo);
+    tmem_st16(tFar + lanes, hi);
+    tmem_st16(tFar + FAR / 2 + lanes, lo);
     tmem_wait_st();
   };
   auto mma_far_scores = [&](int chunk) {                      // phi(Q) phi(K_far)^T: hi hi, lo hi, hi lo
@@ -689,12 +707,13 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       const uint64_t b0 = kmajor_base_h(smem_u32(spare(2)) + (term == 2 ? FAR * 128 : 0));
 #pragma unroll
       for (int k = 0; k < 8; ++k)
-        mma_bf16(tO + 64, (k < 4 ? a0 : a1) + kstep_k(k & 3, HALF_BYTES), b0 + kstep_k(k, HT_HALF), idesc, (term > 0 || k > 0) ? 1u : 0u);
+        mma_bf16(tFar, (k < 4 ? a0 : a1) + kstep_k(k & 3, HALF_BYTES), b0 + kstep_k(k, HT_HALF), idesc, (term > 0 || k > 0) ? 1u : 0u);
     }
   };
 
 
   uint2 v_far[FAR / 4];
+  float window_scale = 0.f;                                  // one-CTA path: of this thread's row
   if (row_warp) {
     // the window output leaves the accumulator
     const uint64_t bad0 = (uint64_t)bars->bad[1] << 32 | bars->bad[0], bad1 = (uint64_t)bars->bad[3] << 32 | bars->bad[2];
@@ -729,18 +748,17 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
 #pragma unroll
         for (int i = 0; i < 32; ++i) ss += (o[i] * inv) * (o[i] * inv);
       }
-      const float f = PARK * inv * rsqrtf(ss * (1.f / TILE) + d.eps);
-      bars->odd[tid] = !(ss < INFINITY);                     // (NaN too: the row is then NaN)
+      window_scale = inv * rsqrtf(ss < INFINITY ? ss * (1.f / TILE) + d.eps : __uint_as_float(0x7fc00000u));   // not finite: NaN
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         float o[32];
         tmem_ld32(tO + lanes + 32 * c, o);
         tmem_wait_ld();
-        uint32_t h[16];
+        uint32_t a16[16], a8[8];                             // 24 words over columns that have been read
 #pragma unroll
-        for (int i = 0; i < 16; ++i)                         // the low bits of 1.5 2^23 + n are those of n
-          h[i] = __byte_perm(__float_as_uint(fmaf(o[2 * i], f, 12582912.f)), __float_as_uint(fmaf(o[2 * i + 1], f, 12582912.f)), 0x5410);
-        tmem_st16(tO + lanes + 16 * c, h);
+        for (int i = 0; i < 8; ++i) pack24(o + 4 * i, &a16[2 * i], &a16[2 * i + 1], &a8[i]);
+        tmem_st16(tO + lanes + 24 * c, a16);
+        tmem_st8(tO + lanes + 24 * c + 16, a8);
       }
       tmem_wait_st();
     }
@@ -809,7 +827,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     __syncthreads();
     tc_fence_after();
     if (warp == 4) {
-      mma_weights(tS, tO + 64, smem_u32(spare(2)), true, steps_of(chunk));
+      mma_weights(tS, tFar, FAR / 2, smem_u32(spare(2)), true, steps_of(chunk));
       mma_commit(&bars->done);
     }
     wait_done();
@@ -881,6 +899,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
   } else {
    auto at_row = [&](int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 15)) << 4)); };
+   auto at_third = [&](int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); };
    if (row_warp) {
     float ss = 0.f;
 #pragma unroll 1
@@ -892,13 +911,19 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       for (int i = 0; i < 32; ++i) ss += (o[i] * inv_phi) * (o[i] * inv_phi);
     }
     const float f = inv_phi * rsqrtf(ss * (1.f / TILE) + d.eps);
-    // the window branch as it was parked, rows of 256 bytes over Q; the linear one, normalised, fp32 rows over slots 0 - 3
+    // the window branch as it was packed, two words of each three in rows of 256 bytes over Q, the third in rows of 128 over slot 4; the
+    // linear one, normalised, fp32 rows over slots 0 - 3
+    bars->window_scale[tid] = window_scale;                  // (nobody looks for parents or far nodes any more)
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
-      float o[32], s16[16];
+      float o[32], s16[16], s8[8];
       tmem_ld32(tS + lanes + 32 * c, o);
-      tmem_ld16(tO + lanes + 16 * c, s16);
+      tmem_ld16(tO + lanes + 24 * c, s16);
+      tmem_ld8(tO + lanes + 24 * c + 16, s8);
       tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *reinterpret_cast<float4*>(slots + 4 * HT_BYTES + at_third(tid, 2 * c + i)) = make_float4(s8[4 * i], s8[4 * i + 1], s8[4 * i + 2], s8[4 * i + 3]);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<uint4*>(smem + at_row(tid, 4 * c + i)) =
@@ -931,12 +956,13 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       for (int k = k0_; i + G * k < it.rows; k += DA_THREADS / 32, out += step) {
         const int r = i + G * k;
         if (bars->depth[n0 + wrap + k] < 0) continue;
-        const short4 u = *reinterpret_cast<const short4*>(smem + at_row(r, lane >> 1) + (lane & 1) * 8);
-        const float4 y = *reinterpret_cast<const float4*>(slots + at_ox(r, lane));
-        const float unit = bars->odd[r] ? __uint_as_float(0x7fc00000u) : 1.f / PARK;
+        const uint2 u = *reinterpret_cast<const uint2*>(smem + at_row(r, lane >> 1) + (lane & 1) * 8);
+        const uint32_t u2 = *reinterpret_cast<const uint32_t*>(slots + 4 * HT_BYTES + at_third(r, lane >> 2) + (lane & 3) * 4);
+        const float4 y = *reinterpret_cast<const float4*>(slots + at_ox(r, lane)), x = unpack24(u.x, u.y, u2);
+        const float f = bars->window_scale[r];
         *reinterpret_cast<uint2*>(out) =
-            make_uint2(pack_bf16(gs.x * ((float)u.x * unit) + gr.x * y.x, gs.y * ((float)u.y * unit) + gr.y * y.y),
-                       pack_bf16(gs.z * ((float)u.z * unit) + gr.z * y.z, gs.w * ((float)u.w * unit) + gr.w * y.w));
+            make_uint2(pack_bf16(gs.x * (x.x * f) + gr.x * y.x, gs.y * (x.y * f) + gr.y * y.y),
+                       pack_bf16(gs.z * (x.z * f) + gr.z * y.z, gs.w * (x.w * f) + gr.w * y.w));
       }
       gs = gs_next;
       gr = gr_next;
