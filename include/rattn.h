@@ -444,8 +444,8 @@ int rattn_qk_prologue_status(void* stream);
  *                with the deepest node's depth, at most 2^31 - 1 - w.
  *   path, n_accepted   rattn_draft_commit only, as rattn_draft_verify writes them.
  * dtype, scale, eps, gains, feature_map, layout and flags (RATTN_FLAG_FORCE_GENERIC) as in rattn_params.  Every
- * combination of dtype, d, w and group is supported; accumulation, softmax, feature map and norms are fp32, and the bf16
- * kernels put no restriction on the range of v.
+ * combination of dtype, d, w and group is supported; accumulation, softmax, feature map and norms are fp32.  v may have any
+ * size as long as the two branches' sums stay within fp32 (the sums of squares of the norms are scaled where they would not).
  */
 typedef struct rattn_draft_params {
   const void* q;

@@ -25,17 +25,6 @@ namespace {
 
 constexpr int DG_WARPS = 4;
 
-__device__ __forceinline__ float wmax(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
-}
-__device__ __forceinline__ float wsum(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
-}
-
 template <typename T> struct Vec;              // 16 bytes of a row as fp32
 template <> struct Vec<float> {
   static constexpr int N = 4;
@@ -269,14 +258,9 @@ __global__ void __launch_bounds__(DG_WARPS * 32) draft_generic_kernel(const __gr
   for (int k = 0; k < RW; ++k) {
     if (e[k] < 0) continue;                                  // (the same for the warp)
     const int n = (row0 + k) / a.group, h = hk * a.group + (row0 + k) % a.group;
-    float so = 0.f, sr = 0.f;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      o[k][i] /= l[k];
-      so += o[k][i] * o[k][i];
-      sr += r[k][i] * r[k][i];
-    }
-    const float is = rsqrtf(wsum(so) / D + a.eps), ir = rsqrtf(wsum(sr) / D + a.eps);
+    for (int i = 0; i < C; ++i) o[k][i] /= l[k];
+    const float is = row_inv_rms(o[k], a.eps), ir = row_inv_rms(r[k], a.eps);
     T* out = static_cast<T*>(a.out) + node_at(a, b, h, a.H_q, n);
 #pragma unroll
     for (int i = 0; i < C; ++i) {

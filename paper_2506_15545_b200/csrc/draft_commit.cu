@@ -18,17 +18,6 @@ namespace {
 
 constexpr int DC_THREADS = 256, DC_TOKENS = DC_THREADS / 32;        // tokens whose phi(k), v lie in shared memory at a time
 
-__device__ __forceinline__ float wmax(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
-}
-__device__ __forceinline__ float wsum(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
-}
-
 template <typename T, int D, int CS>
 __global__ void __launch_bounds__(DC_THREADS, CS == 1 ? 2 : 4) draft_commit_kernel(const __grid_constant__ DraftArgs a) {
   constexpr int C = D / 32, CG = D / 4, LANES = DC_THREADS / CG, ROWS = D / CS / LANES;

@@ -62,6 +62,33 @@ __device__ __forceinline__ void node_path(const int* par, int i, NodeSet* s) {
   }
 }
 
+__device__ __forceinline__ float wmax(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float wsum(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// 1 / sqrt(mean(x^2) + eps) of a row of 32 C values, C of them in each lane.  Squares are summed in fp32, which ends at values of
+// some 1e18: a row whose sum overflows is summed again from values scaled down by kDown, eps likewise.
+constexpr float kDown = 0x1p-100f;
+template <int C>
+__device__ __forceinline__ float row_inv_rms(const float (&x)[C], float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < C; ++i) s += x[i] * x[i];
+  s = wsum(s);
+  if (s != INFINITY) return rsqrtf(s / (32 * C) + eps);
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < C; ++i) s += (x[i] * kDown) * (x[i] * kDown);
+  return rsqrtf(wsum(s) / (32 * C) + eps * kDown * kDown) * kDown;
+}
+
 cudaError_t launch_generic(const DraftArgs& a, cudaStream_t s);
 cudaError_t launch_commit(const DraftArgs& a, cudaStream_t s);
 // The tensor-core kernel and its status word (RATTN_ERR_TIMEOUT once a bounded wait has expired; reading clears it).

@@ -78,16 +78,6 @@ struct alignas(64) TcMaps {
   UMap k, v;                             // the nodes' tensors, box 64 columns x 64 nodes
 };
 
-__device__ __forceinline__ float wmax(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
-}
-__device__ __forceinline__ float wsum(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
-}
 __device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }   // bits < n
 __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
@@ -711,6 +701,31 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
     }
   };
 
+  // What the row in this thread's lane of an accumulator, `by` times it being a branch's output, is to be multiplied by: by / rms.
+  // A sum of squares that overflows is formed again from values scaled down (row_inv_rms).
+  auto norm_scale = [&](uint32_t at, float by) {
+    float scale = by, down = 1.f;
+#pragma unroll 1
+    for (;;) {
+      float ss = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        tmem_ld32(at + lanes + 32 * c, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) ss += (o[i] * scale) * (o[i] * scale);
+      }
+      const float f = scale * rsqrtf(ss * (1.f / TILE) + d.eps * down * down);
+      const bool again = down == 1.f && ss == INFINITY;
+      if (!__any_sync(0xffffffffu, again)) return f;
+      // (rows that stay as they are keep their scale and are summed along)
+      if (again) {
+        down = kDown;
+        scale = by * kDown;
+      }
+    }
+  };
 
   uint2 v_far[FAR / 4];
   float window_scale = 0.f;                                  // one-CTA path: of this thread's row
@@ -739,16 +754,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       }
     } else {
       const float inv = (seen ? __uint_as_float(0x7fc00000u) : 1.f) / l;
-      float ss = 0.f;
-#pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        float o[32];
-        tmem_ld32(tO + lanes + 32 * c, o);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) ss += (o[i] * inv) * (o[i] * inv);
-      }
-      window_scale = inv * rsqrtf(ss < INFINITY ? ss * (1.f / TILE) + d.eps : __uint_as_float(0x7fc00000u));   // not finite: NaN
+      window_scale = norm_scale(tO, inv);
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         float o[32];
@@ -883,34 +889,24 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
       }
       const float m = wmax(m_r), f = ex2(m_r - (m == -INFINITY ? 0.f : m));
       const float inv = 1.f / wsum(lane < CS ? f * l_r : 0.f);
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+      float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         if (k < CS) {
           const float fr = __shfl_sync(0xffffffffu, f, k) * inv;
-          x.x += fr * p[k].x; x.y += fr * p[k].y; x.z += fr * p[k].z; x.w += fr * p[k].w;
-          y.x += q[k].x; y.y += q[k].y; y.z += q[k].z; y.w += q[k].w;
+          x[0] += fr * p[k].x; x[1] += fr * p[k].y; x[2] += fr * p[k].z; x[3] += fr * p[k].w;
+          y[0] += q[k].x; y[1] += q[k].y; y[2] += q[k].z; y[3] += q[k].w;
         }
-      const float ss = wsum(x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w), sr = wsum(y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w);
-      const float is = rsqrtf(ss / TILE + d.eps), ir = rsqrtf(sr / TILE + d.eps);
+      const float is = row_inv_rms(x, d.eps), ir = row_inv_rms(y, d.eps);
       *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(d.out) + node_at(d, it.b, h, d.H_q, n) + c0) =
-          make_uint2(pack_bf16(gs.x * x.x * is + gr.x * y.x * ir, gs.y * x.y * is + gr.y * y.y * ir),
-                     pack_bf16(gs.z * x.z * is + gr.z * y.z * ir, gs.w * x.w * is + gr.w * y.w * ir));
+          make_uint2(pack_bf16(gs.x * x[0] * is + gr.x * y[0] * ir, gs.y * x[1] * is + gr.y * y[1] * ir),
+                     pack_bf16(gs.z * x[2] * is + gr.z * y[2] * ir, gs.w * x[3] * is + gr.w * y[3] * ir));
     }
   } else {
    auto at_row = [&](int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 15)) << 4)); };
    auto at_third = [&](int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); };
    if (row_warp) {
-    float ss = 0.f;
-#pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
-      float o[32];
-      tmem_ld32(tS + lanes + 32 * c, o);
-      tmem_wait_ld();
-#pragma unroll
-      for (int i = 0; i < 32; ++i) ss += (o[i] * inv_phi) * (o[i] * inv_phi);
-    }
-    const float f = inv_phi * rsqrtf(ss * (1.f / TILE) + d.eps);
+    const float f = norm_scale(tS, inv_phi);
     // the window branch as it was packed, two words of each three in rows of 256 bytes over Q, the third in rows of 128 over slot 4; the
     // linear one, normalised, fp32 rows over slots 0 - 3
     bars->window_scale[tid] = window_scale;                  // (nobody looks for parents or far nodes any more)

@@ -51,3 +51,24 @@ def test_rows_far_below_eps_and_large_gains(B, H, d, dtype, flags, size, eps, ga
     s.hist = [[k, v * f] for k, v in s.hist]
     s.gs = s.gs * gain
     run_and_check(s, eps, flags, (0, B - 1))
+
+
+@pytest.mark.parametrize("B,H,d,dtype,flags", PLANS)
+@pytest.mark.parametrize("size", [58, 64, 90, 115])
+def test_values_whose_squares_leave_fp32(B, H, d, dtype, flags, size):
+    """The norms cancel a factor common to all values, up to where the sums of values themselves leave fp32 (2^128; here they
+    are below 2^7 times the factor: the state of 60 tokens times a feature map of at most 1)."""
+    s = Setup(B, H, H, 5, d, 40, dtype, 100, "tree", seed=32)
+    f = 2.0 ** size
+    s.v, s.v_ring, s.state = s.v * f, s.v_ring * f, s.state * f
+    s.hist = [[k, v * f] for k, v in s.hist]
+    run_and_check(s, 1e-6, flags, (0, B - 1))
+
+
+@pytest.mark.parametrize("B,H,d,dtype,flags", PLANS)
+def test_one_node_of_large_values(B, H, d, dtype, flags):
+    """Rows that see the node overflow, their neighbours do not; an eps of that size counts."""
+    s = Setup(B, H, H, 6, d, 40, dtype, 100, "star", seed=33)
+    s.v[:, :, 2] *= 2.0 ** 70
+    run_and_check(s, 1e-6, flags, (0, B - 1))
+    run_and_check(s, 2.0 ** 127, flags, (0, B - 1))
