@@ -441,7 +441,8 @@ int rattn_qk_prologue_status(void* stream);
  *   k_ring, v_ring [B,H_kv,w,d], state [B,H_kv,d,d] fp32, pos: as for rattn_decode_step: the ring holds the tokens
  *                pos-w .. pos-1 (those >= 0) at slot j % w, the state those before.
  *   pos_dev      optional device int32 [B], a position per batch entry (overrides pos).  Positions are at least 0 and,
- *                with the deepest node's depth, at most 2^31 - 1 - w.
+ *                with the deepest node's depth, at most 2^31 - 1 - w (of a position that is given by value, without the
+ *                depth, this is checked).
  *   path, n_accepted   rattn_draft_commit only, as rattn_draft_verify writes them.
  * dtype, scale, eps, gains, feature_map, layout and flags (RATTN_FLAG_FORCE_GENERIC) as in rattn_params.  Every
  * combination of dtype, d, w and group is supported; accumulation, softmax, feature map and norms are fp32.  v may have any

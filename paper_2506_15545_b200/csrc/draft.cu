@@ -302,7 +302,7 @@ int resolve(const rattn_draft_params* p, DraftArgs* a) {
   if (!p) return RATTN_ERR_NULL_PTR;
   if (p->B < 1 || p->H_q < 1 || p->H_kv < 1 || p->N < 1 || p->N > kMaxNodes || p->w < 1) return RATTN_ERR_BAD_ARG;
   if (p->H_q % p->H_kv != 0) return RATTN_ERR_BAD_ARG;
-  if (!p->pos_dev && (p->pos < 0 || (long long)p->pos + kMaxNodes + p->w > 0x7fffffffll)) return RATTN_ERR_BAD_ARG;
+  if (!p->pos_dev && (p->pos < 0 || (long long)p->pos + p->w > 0x7fffffffll)) return RATTN_ERR_BAD_ARG;
   // row and slot counts stay below 2^31
   if ((long long)p->B * p->H_q * p->N >= (1ll << 31) || (long long)p->B * p->H_kv * p->w >= (1ll << 31) ||
       (long long)p->B * p->H_kv >= (1ll << 28))

@@ -182,6 +182,14 @@ def test_draft_commit_refuses(R, kw, code):
     assert R.lib().rattn_draft_commit(None, None) == R.lib().rattn_draft_attention(None, None) == -2
 
 
+@pytest.mark.parametrize("w", [1, 64, 1000])
+def test_every_position_that_is_documented_is_taken(R, w):
+    """2^31 - 1 - w is the last; that a position passes shows in the next check's answer, and nothing is launched."""
+    for call in (R.lib().rattn_draft_attention, R.lib().rattn_draft_commit):
+        for pos, code in ((2 ** 31 - 1 - w, -3), (2 ** 31 - 1 - w - 128, -3), (2 ** 31 - w, -1)):
+            assert call(_draft(R, pos=pos, w=w, k=FAKE + 8), None) == code
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(B=0), -1), (dict(N=0), -1), (dict(N=129), -1), (dict(V=0), -1), (dict(V=2 ** 31 - 1), -1), (dict(dtype=2), -4),
     (dict(tokens=0), -2), (dict(parents=0), -2), (dict(target_probs=0), -2), (dict(u=0), -2), (dict(path=0), -2),

@@ -72,3 +72,22 @@ def test_one_node_of_large_values(B, H, d, dtype, flags):
     s.v[:, :, 2] *= 2.0 ** 70
     run_and_check(s, 1e-6, flags, (0, B - 1))
     run_and_check(s, 2.0 ** 127, flags, (0, B - 1))
+
+
+@pytest.mark.parametrize("B,H,d,dtype,flags", PLANS)
+def test_one_node_at_the_last_position(B, H, d, dtype, flags):
+    """At 2^31 - 1 - w: the bits of a small position with the same remainder, from the call and from the commit."""
+    w = 100
+    s = Setup(B, H, H, 1, d, w, dtype, 2 * w + (2 ** 31 - 1) % w, "chain", seed=34)
+    top = 2 ** 31 - 1 - w
+    par, one = torch.zeros(B, 1, dtype=torch.int32, device="cuda") - 1, torch.ones(B, dtype=torch.int32, device="cuda")
+    q, k, v = (x.cuda() for x in (s.q, s.k, s.v))
+    got = []
+    for pos in (s.pos[0], top):
+        cache = [s.k_ring.clone(), s.v_ring.clone(), s.state.clone()]
+        y = R.rattn_draft_attention(q, k, v, par, *cache, pos, scale=s.scale, flags=flags)
+        R.rattn_draft_commit(k, v, par + 1, one, *cache, pos)
+        got.append([y] + cache)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    with pytest.raises(R.RattnError):
+        R.rattn_draft_attention(q, k, v, par, *cache, top + 1, scale=s.scale, flags=flags)
