@@ -77,7 +77,7 @@ __device__ __forceinline__ AxesPlace place_of(const QkArgs& a, const AxesFreqs& 
   AxesPlace p;
   const int* at = f.at + (size_t)b * a.T + t;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) p.at[x] = x < f.n_axes ? __ldg(at + x * f.tokens) : 0;
+  for (int x = 0; x < 4; ++x) p.at[x] = x < f.n_axes ? at[x * f.tokens] : 0;
   return p;
 }
 __device__ __forceinline__ float angle(const Freqs& f, int i, const Place& p) { return reduced((double)p.at * f.inv[i]); }
@@ -344,7 +344,7 @@ qk_prologue_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ typ
       for (int tok = tid / (D / 2); tok < n_tok; tok += STEP * AHEAD) {
         int x[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) x[j] = __ldg(at + min(tok + j * STEP, n_tok - 1));
+        for (int j = 0; j < AHEAD; ++j) x[j] = at[min(tok + j * STEP, n_tok - 1)];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
           if (tok + j * STEP < n_tok) {
