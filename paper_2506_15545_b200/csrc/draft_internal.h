@@ -89,6 +89,35 @@ __device__ __forceinline__ float row_inv_rms(const float (&x)[C], float eps) {
   return rsqrtf(wsum(s) / (32 * C) + eps * kDown * kDown) * kDown;
 }
 
+// How many clusters of `cluster` CTAs (2, 4 or 8) of the kernel run at once on the current device, asked of the driver once per
+// device.  Fewer than its SMs have room for: a cluster lies within one GPC, and what is left of a GPC takes none.
+template <auto Kernel>
+cudaError_t clusters_at_once(int cluster, int threads, int smem, int* n) {
+  static std::atomic<int> known[kMaxDevices][4];             // 1 more than the answer
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::atomic<int>& slot = known[dev][cluster >> 2 ? (cluster >> 3) + 2 : 1];
+  if (const int k = slot.load(std::memory_order_relaxed)) {
+    *n = k - 1;
+    return cudaSuccess;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)cluster);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(n, Kernel, &cfg);
+  if (e == cudaSuccess) slot.store(*n + 1, std::memory_order_relaxed);
+  return e;
+}
+
 cudaError_t launch_generic(const DraftArgs& a, cudaStream_t s);
 cudaError_t launch_commit(const DraftArgs& a, cudaStream_t s);
 // The tensor-core kernel and its status word (RATTN_ERR_TIMEOUT once a bounded wait has expired; reading clears it).

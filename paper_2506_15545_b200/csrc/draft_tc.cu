@@ -20,7 +20,7 @@
 // rounded to the upper 24 bits of its fp32 form, off by 2^-17 of itself whatever the row's size, eps or gain.  y leaves through
 // shared memory, a warp per row, where gains are read once per row and coalesced.
 //
-// Few heads (B H_kv row tiles below the SMs): a cluster of CTAs shares the tiles of keys and the features of S; the partial
+// Few heads (B H_kv row tiles that find room as clusters): a cluster of CTAs shares the tiles of keys and the features of S; the partial
 // outputs (fp32) meet through distributed shared memory, a warp per row.
 //
 // A node with a value that is not finite is cleared in the tile (its zero weight would spread it over all rows) and makes the
@@ -1030,16 +1030,21 @@ cudaError_t launch_tc(const DraftArgs& d, cudaStream_t s) {
       !make_user_map(&m.k, d.k, (uint64_t)d.N, (uint64_t)d.H_kv, (uint64_t)d.B, d.layout, 64) ||
       !make_user_map(&m.v, d.v, (uint64_t)d.N, (uint64_t)d.H_kv, (uint64_t)d.B, d.layout, 64))
     return cudaErrorInvalidValue;
-  int n_sm = 0;
-  const cudaError_t e = sm_count(&n_sm);
-  if (e != cudaSuccess) return e;
   const long long R = (long long)d.group * d.N, heads = (long long)d.B * d.H_kv;
   const int tiles = ((d.pos_dev || d.pos >= d.w ? d.w : d.pos) + 63) / 64 + (d.N + 63) / 64;
-  // Row tiles of a cluster hold at most 96 rows (what the exchange has room for); a cluster has as many CTAs as still find an
-  // SM each, and no more than there are tiles of keys.
+  // Row tiles of a cluster hold at most 96 rows (what the exchange has room for); a cluster has as many CTAs as let all clusters run
+  // at once, and no more than there are tiles of keys (4 query heads x 6 nodes per K/V head, w = 512; CTAs per cluster 1 / 2 / 4 / 8:
+  // 15 heads 22.0 / 16.8 / 14.7 / 14.0 us, 16 heads 22.1 / 16.9 / 14.4 / 25.8 where 15 clusters of eight run at once; 33 of four: 36
+  // heads 23.1 / 17.2 / 28.6; 74 of two: 74 heads 21.2 / 19.0, 75 heads 22.9).
   const long long rt_c = (R + DA_CLUSTER_ROWS - 1) / DA_CLUSTER_ROWS;
-  int cs = 1;
-  while (cs < 8 && 2 * cs <= tiles && heads * rt_c * 2 * cs <= n_sm) cs *= 2;
+  int cs = 1, fit = 0;
+  cudaError_t e = allow_smem<draft_tc_kernel<true>>(DA_SMEM_CLUSTER);
+  while (e == cudaSuccess && cs < 8 && 2 * cs <= tiles) {
+    e = clusters_at_once<draft_tc_kernel<true>>(2 * cs, DA_THREADS, DA_SMEM_CLUSTER, &fit);
+    if (heads * rt_c > fit) break;
+    cs *= 2;
+  }
+  if (e != cudaSuccess) return e;
   a.cluster = cs;
   a.row_tiles = (int)(cs > 1 ? rt_c : (R + TILE - 1) / TILE);
   a.rows_per_tile = (int)((R + a.row_tiles - 1) / a.row_tiles);

@@ -113,3 +113,37 @@ def test_portable_attention_with_four_rows_to_a_warp(Hq, d, dtype, N, w, kind, p
             # fp32 arithmetic: the framework's bound for fp32 outputs, 1e-4, and the rounding of the output
             bound = 1e-4 + (2.0 ** -8 if dtype == "bf16" else 0.0) * np.abs(ref[rows])
             assert (np.abs(y[b][rows] - ref[rows]) <= bound).all(), b
+
+
+@pytest.mark.parametrize("heads", [14, 15, 16, 18, 32, 33, 34, 37, 38, 73, 74, 75, 80])
+def test_attention_around_the_cluster_sizes(heads):
+    """As many heads as clusters of eight, four, two CTAs run at once, and one more: the same rows as the portable kernel's."""
+    B, G, N, d, w, pos = heads, 4, 6, 128, 320, 1000
+    g = torch.Generator(device="cuda").manual_seed(heads)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    q, k, v, kr, vr = (rnd(*s).bfloat16() for s in ((B, G, N, d), (B, 1, N, d), (B, 1, N, d), (B, 1, w, d), (B, 1, w, d)))
+    state = 5 * rnd(B, 1, d, d)
+    par = torch.tensor([[-1, 0, 0, 1, 3, 2]] * B, dtype=torch.int32, device="cuda")
+    a, b = (R.rattn_draft_attention(q, k, v, par, kr, vr, state, pos, scale=d ** -0.5, flags=f).float() for f in (0, R.FLAG_FORCE_GENERIC))
+    assert R.rattn_draft_status() == 0
+    # each rounds an output once, to 2^-8 of it at most, from values that are 2^-10 apart at most
+    assert ((a - b).abs() <= 2 * (2.0 ** -8 * b.abs() + 2.0 ** -10)).all()
+
+
+@pytest.mark.parametrize("heads", [141, 142, 143, 147, 148, 149, 300])
+def test_commit_around_the_cluster_sizes(heads):
+    """Tokens are added in order whatever shares a head: the bits of the same entries in calls of a few."""
+    B, N, d, w, pos = heads, 12, 128, 8, 50
+    g = torch.Generator(device="cuda").manual_seed(heads)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    k, v, kr, vr = (rnd(*s).bfloat16() for s in ((B, 1, N, d), (B, 1, N, d), (B, 1, w, d), (B, 1, w, d)))
+    state = rnd(B, 1, d, d)
+    path = torch.stack([torch.randperm(N, device="cuda", generator=g) for _ in range(B)]).int()
+    n = torch.randint(0, N + 1, (B,), device="cuda", generator=g, dtype=torch.int32)
+    whole, parts = [kr.clone(), vr.clone(), state.clone()], [kr.clone(), vr.clone(), state.clone()]
+    R.rattn_draft_commit(k, v, path, n, *whole, pos)
+    for i in range(0, B, 50):
+        at = slice(i, i + 50)
+        R.rattn_draft_commit(k[at], v[at], path[at], n[at], *(x[at] for x in parts), pos)
+    assert all(torch.equal(a, b) for a, b in zip(whole, parts))
+    assert not torch.equal(whole[2], state)
