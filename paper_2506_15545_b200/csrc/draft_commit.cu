@@ -5,7 +5,7 @@
 // old(a) = token pos + a - w: a ring slot's for a < w, an accepted token's behind that.  One read and one write of the
 // state (64 KB each at d = 128) is nearly all of the traffic, so HBM bounds it, or latency for few heads: a CTA has its share
 // of the state's rows in registers, requested before anything else, and the ring rows that the first eight tokens would push
-// out are requested before it is known how many tokens there are.  Few heads are shared by clusters of four CTAs.
+// out are requested before it is known how many tokens there are.  Few heads of d = 128 are shared by clusters of four CTAs.
 // Tokens are added in order, as single steps would (fp32).
 //
 // The slots that the new tokens take are those that the old ones leave: the CTAs of a head meet at a barrier between the last
@@ -137,14 +137,18 @@ cudaError_t launch_commit_cs(const DraftArgs& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-// A head to a cluster of four CTAs while there are no more heads than SMs, to one CTA beyond (d = 128, bf16; one CTA / four:
-// 8 heads 4.1 / 3.6 us, 128 heads 5.8 / 5.3, 256 heads 6.5 / 9.4, 512 heads 11.2 / 16.9: the state's 67 MB at 5.9 TB/s).
+// d = 128: a head to a cluster of four CTAs while all of these run at once, to one CTA beyond; d = 64, with a quarter of the
+// state: one CTA.  One CTA / four, bf16, states from HBM: d = 128, 8 heads 3.7 / 3.5 us, 64 6.6 / 5.9, 128 7.6 / 7.0, 148 6.7 / 9.8,
+// 512 16.8 / 21.7 (the state's 67 MB at 4.1 TB/s; 1600 heads: 5.3); d = 64, 8 heads 2.4 / 2.8, 128 4.1 / 4.6, 512 8.1 / 15.7.
 template <typename T, int D>
 cudaError_t launch_commit_as(const DraftArgs& a, cudaStream_t s) {
-  int n_sm = 0;
-  const cudaError_t e = sm_count(&n_sm);
-  if (e != cudaSuccess) return e;
-  return a.B * a.H_kv <= n_sm ? launch_commit_cs<T, D, 4>(a, s) : launch_commit_cs<T, D, 1>(a, s);
+  if constexpr (D == 128) {
+    int n = 0;
+    const cudaError_t e = clusters_at_once<draft_commit_kernel<T, D, 4>>(4, DC_THREADS, 0, &n);
+    if (e != cudaSuccess) return e;
+    if (a.B * a.H_kv <= n) return launch_commit_cs<T, D, 4>(a, s);
+  }
+  return launch_commit_cs<T, D, 1>(a, s);
 }
 
 }  // namespace
