@@ -284,14 +284,35 @@ cudaError_t launch_generic_rows(const DraftArgs& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-// Four rows to a warp share its reads of keys and values; where that leaves SMs without a CTA, one.
+// How many CTAs of one row to a warp run at once on the current device, asked of the driver once per device.
+template <typename T, int D>
+cudaError_t one_row_ctas_at_once(int* n) {
+  static std::atomic<int> known[kMaxDevices];
+  constexpr int smem = GenericPlan<D, 1>::END * (int)sizeof(float);
+  int dev = 0, n_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  if ((*n = known[dev].load(std::memory_order_relaxed)) != 0) return cudaSuccess;
+  e = allow_smem<draft_generic_kernel<T, D, 1>>(smem);
+  if (e == cudaSuccess) e = sm_count(&n_sm);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(n, draft_generic_kernel<T, D, 1>, DG_WARPS * 32, (size_t)smem);
+  *n *= n_sm;
+  if (e == cudaSuccess) known[dev].store(*n, std::memory_order_relaxed);
+  return e;
+}
+
+// A row to a warp while all CTAs of that run at once: a wave takes half of the time of one of four rows to a warp, which share
+// the warp's reads of keys and values and win from the second wave on.  One / four, w = 512, fp32: d = 128 (740 CTAs at
+// once), 560 CTAs 137 / 201 us, 888 259 / 196, 7680 1373 / 804; d = 64 (1184), 1120 95 / 137, 1536 148 / 116, 7680 591 / 402.
+// (w = 100: 1776 CTAs of a head's 192 rows 69 / 85, 7680 231 / 201.)
 template <typename T, int D>
 cudaError_t launch_generic_as(const DraftArgs& a, cudaStream_t s) {
-  int n_sm = 0;
-  const cudaError_t e = sm_count(&n_sm);
+  int n = 0;
+  const cudaError_t e = one_row_ctas_at_once<T, D>(&n);
   if (e != cudaSuccess) return e;
-  const long long ctas = (long long)a.B * a.H_kv * ((a.group * a.N + 4 * DG_WARPS - 1) / (4 * DG_WARPS));
-  return ctas >= n_sm ? launch_generic_rows<T, D, 4>(a, s) : launch_generic_rows<T, D, 1>(a, s);
+  const long long ctas = (long long)a.B * a.H_kv * ((a.group * a.N + DG_WARPS - 1) / DG_WARPS);
+  return ctas <= n ? launch_generic_rows<T, D, 1>(a, s) : launch_generic_rows<T, D, 4>(a, s);
 }
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }

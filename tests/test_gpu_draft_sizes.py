@@ -97,8 +97,9 @@ def test_commit_of_more_heads_than_sms(d, dtype, layout, phi):
     (8, 128, "f32", 16, 64, "star"),
 ])
 def test_portable_attention_with_four_rows_to_a_warp(Hq, d, dtype, N, w, kind, phi):
-    """More K/V heads than SMs, each entry at a position of its own; rows against the oracle, for some entries."""
-    B, Hkv = 20, 8
+    """More CTAs of one row to a warp than run at once, each entry at a position of its own; rows against the oracle, for some
+    entries."""
+    B, Hkv = 80, 8
     pos = np.random.default_rng(N).integers(0, 3 * w, B)
     pos[0], pos[1], pos[-1] = 0, w, 3 * w
     s = Setup(B, Hq, Hkv, N, d, w, dtype, pos.tolist(), kind, phi=phi, seed=N)
