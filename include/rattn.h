@@ -445,7 +445,9 @@ int rattn_qk_prologue_status(void* stream);
  *                depth, this is checked).
  *   path, n_accepted   rattn_draft_commit only, as rattn_draft_verify writes them.
  * dtype, scale, eps, gains, feature_map, layout and flags (RATTN_FLAG_FORCE_GENERIC) as in rattn_params.  Every
- * combination of dtype, d, w and group is supported; accumulation, softmax, feature map and norms are fp32.  v may have any
+ * combination of dtype, d, w and group is supported; accumulation, softmax, feature map and norms are fp32.  Where bf16, d = 128 and
+ * scale > 0 go to the tensor cores, softmax weights, feature maps and the state enter their products as pairs of bf16 values, which
+ * keep 16 bits of each.  v may have any
  * size as long as the two branches' sums stay within fp32 (the sums of squares of the norms are scaled where they would not).
  */
 typedef struct rattn_draft_params {
@@ -490,8 +492,8 @@ int rattn_draft_attention(const rattn_draft_params* p, void* stream);
  */
 int rattn_draft_commit(const rattn_draft_params* p, void* stream);
 
-/* RATTN_ERR_TIMEOUT if a bounded device-side wait has expired in any of the draft calls on the current device since it
- * was last asked (synchronises the stream), else RATTN_OK. */
+/* RATTN_ERR_TIMEOUT if a bounded device-side wait has expired in a draft call (of which the attention alone has any) on the current
+ * device since it was last asked (synchronises the stream), else RATTN_OK. */
 int rattn_draft_status(void* stream);
 
 /*

@@ -13,8 +13,8 @@
 // The portable kernel: four warps walk tiles of 32 keys, which they load together into shared memory, a warp for one or four rows.
 // A lane forms the scores of its key for the warp's rows, then the lanes hold the features and add the values of those keys that a row
 // sees, one by one -- what it does not see is not multiplied, so NaN or infinity there stays there.  It is bound by its
-// shared-memory loads and the latency of a tile (16 heads x 64 rows, d = 64, w = 512, fp32: 54 us; with every lane reading
-// its key's row from global memory 168 us).
+// shared-memory loads and the latency of a tile (16 heads x 64 rows, d = 64, w = 512, fp32: 61 us, 54 with everything
+// in L2; there with every lane reading its key's row from global memory 168).
 #include <cmath>
 
 #include "draft_internal.h"

@@ -451,7 +451,7 @@ draft_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ TcMaps
   };
   // Half of S (128 threads, 16 float4 each), split, to the last two spare slots.  A CTA of many loads its second half and keeps it
   // while the first is multiplied; in a cluster there is one half, of which each CTA has a part, and eight loads at a time are
-  // the smaller code (a chain of 6 for one sequence: 12.9 against 13.6 us; elsewhere 4 % slower).
+  // the smaller code (a chain of 6 for one sequence, inputs in L2: 12.9 against 13.6 us; elsewhere 4 % slower).
   constexpr int S_AHEAD = CL ? 8 : 16;
   float4 x_s[S_AHEAD];
   auto load_s = [&](int hh, int i0) {
