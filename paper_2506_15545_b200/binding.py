@@ -5,6 +5,10 @@ nothing but turn torch tensors into device pointers, sizes and a stream handle. 
 that enqueue work are marshalled by the extension csrc/native.cpp (a decode step is over
 before ctypes has filled its parameter block); queries go through ctypes.  There is no
 fallback: if the library or the extension has not been built, loading it raises.
+
+Where a `stream` is given, the call runs there, and what it allocates belongs to that stream
+as it would under torch.cuda.stream(stream): inputs have to be ready in its order, and a
+result that another stream uses is the caller's to order and to record.
 """
 from __future__ import annotations
 

@@ -58,10 +58,27 @@ void check(int code, const char* where) {
   throw Raised{};
 }
 
+// While it lives, a stream that the caller has named is torch's current one, so that results and workspaces come from memory
+// that is free in the order of that stream: a block from another stream's pool may still be in use there, and a workspace
+// that goes back to it would be given out before the call has run.
+struct StreamScope {
+  c10::optional<c10::cuda::CUDAStream> before;
+  StreamScope() = default;
+  StreamScope(const StreamScope&) = delete;
+  ~StreamScope() {
+    if (before) c10::cuda::setCurrentCUDAStream(*before);
+  }
+  void enter(cudaStream_t s) {
+    before = c10::cuda::getCurrentCUDAStream();
+    c10::cuda::setCurrentCUDAStream(c10::cuda::getStreamFromExternal(s, before->device_index()));
+  }
+};
+
 // Positional arguments of one call, read in order.
 struct Args {
   PyObject* const* at;
   PyObject* const* end;
+  StreamScope scope = {};
   PyObject* next() {
     if (at == end) raise(PyExc_TypeError, "too few arguments");
     return *at++;
@@ -112,6 +129,7 @@ struct Args {
     void* s = PyLong_AsVoidPtr(h);
     Py_DECREF(h);
     if (!s && PyErr_Occurred()) throw Raised{};
+    scope.enter(static_cast<cudaStream_t>(s));
     return s;
   }
 };
@@ -169,7 +187,7 @@ int released(F&& call) {                     // the library call itself runs wit
 template <PyObject* (*F)(Args)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   try {
-    return F(Args{args, args + n});
+    return F(Args{args, args + n, {}});
   } catch (const Raised&) {
   } catch (...) {                            // as torch's own functions raise it: callers catch torch.OutOfMemoryError
     torch::translate_exception_to_python(std::current_exception());
